@@ -370,7 +370,8 @@ glr_status glr_profile_query(glr_handle* h, int32_t group, double* total_ms, int
 const char* glr_status_string(glr_status s);
 
 /* Text of the last error on this handle ("" if none); NULL handle gives the
- * last error of a failed glr_create on this thread. */
+ * last error of a failed glr_create, or of another failed call without a
+ * handle, on this thread. */
 const char* glr_last_error(const glr_handle* h);
 
 #ifdef __cplusplus

@@ -1,0 +1,195 @@
+/*
+ * greedylore_losses.h -- C ABI of the losses over a language model's logits
+ * and their gradients (MI355X, gfx950), in the same library as greedylore.h.
+ *
+ * They make what the compression step takes: the gradient of a loss with
+ * respect to the logits, from which backward fills the layers' gradients.
+ * Every call works on rows of logits z in R^V (`vocab` = V).  With the
+ * temperature T, m = max_j z_j and s = sum_j exp((z_j - m) / T), the
+ * log-probability of a row's target y is
+ *
+ *   lp = (z_y - m) / T - log s,    d lp / d z_j = ([j = y] - exp((z_j - m) / T) / s) / T.
+ *
+ * Rows.  Row (b, s), b < batch, s < steps, of an array with strides
+ * (stride_b, stride_s), in elements, starts at data + b stride_b + s stride_s;
+ * a row's V logits are contiguous.  Row t = b steps + s in what follows.  Any
+ * strides are taken: padded rows, the logits of all positions but the last of
+ * each sequence, arrays broadcast over a sequence (stride 0).  Row pointers
+ * need the alignment of one element only.  Rows of dlogits must not overlap;
+ * dlogits may be the logits themselves (same pointer and strides: the gradient
+ * replaces them) and otherwise must not alias any input.
+ *
+ * Masks.  A row whose target is ignore_index is not trained on: its logits
+ * are not read, it adds nothing to a loss or a count, its log-probability is
+ * written as 0 and its gradient row as zeros.  A target outside [0, V) that is
+ * not ignore_index makes its row NaN (log-probability, loss and gradient; no
+ * memory is read for it); likewise a teacher's index at or above V.  Logits
+ * of -inf have probability 0; a row of nothing but -inf, with +inf or with
+ * NaN is NaN, and only that row.
+ *
+ * Sequences.  cu_seqlens, if not NULL, is a device array of seqs + 1
+ * non-decreasing row offsets: sequence i holds rows cu[i] .. cu[i + 1] - 1
+ * (none, if equal); rows outside every sequence count as masked; offsets are
+ * clamped to the rows there are.  Without it sequence b holds the rows of
+ * batch entry b, and seqs must be `batch`.
+ *
+ * Precision.  Logits and their gradient are fp32, bf16 or fp16; row sums,
+ * log-probabilities and per-row arrays are fp32, what is made of a row's sums
+ * (its log-probability, the terms of a loss, sums over rows) is computed in
+ * fp64.  A gradient element is rounded once, from fp32, as it is stored; it is
+ * d loss / d z times grad_scale.  All sums have a fixed order: the same call
+ * gives the same bits.
+ *
+ * Memory, streams and errors are as in greedylore.h: the caller owns every
+ * buffer; the calls only enqueue, on `stream`, and may be captured into a HIP
+ * graph; they keep nothing between calls.  d_ws is scratch of at least
+ * glr_loss_workspace_bytes bytes, 16-byte aligned, in use until the call's
+ * work has run.  Argument errors are found before anything is enqueued; the
+ * text is glr_last_error(NULL).
+ */
+#ifndef GREEDYLORE_LOSSES_H
+#define GREEDYLORE_LOSSES_H
+
+#include "greedylore.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef enum { GLR_F32 = 0, GLR_BF16 = 1, GLR_F16 = 2 } glr_dtype;
+typedef enum { GLR_I32 = 0, GLR_I64 = 1 } glr_itype;
+
+typedef struct {
+  const void* data;            /* NULL: absent */
+  int64_t stride_b, stride_s;  /* elements */
+} glr_row_array;
+
+typedef struct {
+  int64_t batch, steps;        /* rows: batch * steps < 2^31, each >= 0 */
+  int64_t vocab;               /* V in [1, 2^28] */
+  glr_row_array logits;
+  glr_row_array dlogits;       /* written; data NULL: no gradient */
+  int32_t dtype;               /* glr_dtype of logits and dlogits */
+  int32_t target_type;         /* glr_itype of targets */
+  glr_row_array targets;       /* NULL data: every row is trained on (distillation only) */
+  int64_t ignore_index;
+  double temperature;          /* T, in [2^-20, 2^20] */
+  double grad_scale;           /* finite */
+} glr_loss_rows;
+
+typedef struct {
+  int64_t seqs;
+  const void* cu_seqlens;      /* NULL: the batch entries */
+  int32_t cu_type;             /* glr_itype */
+} glr_loss_seqs;
+
+typedef enum {
+  GLR_LOSS_LOGPROBS = 0,
+  GLR_LOSS_PREFERENCE = 1,
+  GLR_LOSS_POLICY = 2,
+  GLR_LOSS_DISTILL = 3
+} glr_loss_op;
+
+/* Scratch bytes of a call of `op` on these rows (pointers are not looked at;
+ * only whether dlogits.data is NULL); seqs: sequences (0 where it has none).
+ * Pure host. */
+glr_status glr_loss_workspace_bytes(const glr_loss_rows* rows, int32_t op, int64_t seqs, size_t* bytes);
+
+/* Log-probabilities of the targets: logps (fp32, batch x steps contiguous).
+ * stats, if not NULL, receives (m, s) of every row, two fp32 each, for
+ * glr_token_logprobs_backward.  With dlogits, weights (fp32) has to be there and the
+ * gradient of sum_t weights_t lp_t is written in the same pass. */
+glr_status glr_token_logprobs(const glr_loss_rows* rows, const glr_row_array* weights, float* logps,
+                              float* stats, void* d_ws, size_t ws_bytes, void* stream);
+
+/* The gradient of sum_t grad_logps_t lp_t from the stats of the forward call. */
+glr_status glr_token_logprobs_backward(const glr_loss_rows* rows, const float* stats,
+                                       const glr_row_array* grad_logps, void* stream);
+
+/* Preference loss over pairs: sequence p < seqs / 2 is the chosen and
+ * seqs / 2 + p the rejected one of pair p.  With L_i the sum (average != 0:
+ * the mean) of lp over the rows of sequence i that are trained on, and
+ * D = (L_c - ref_c) - (L_r - ref_r), h = beta D:
+ *   SIGMOID  -(1 - label_smoothing) log sigma(h) - label_smoothing log sigma(-h)
+ *   HINGE    max(0, 1 - h)
+ *   SQUARED  (D - 1 / (2 beta))^2
+ * averaged over the pairs.  An empty sequence has L = 0. */
+typedef enum { GLR_PREF_SIGMOID = 0, GLR_PREF_HINGE = 1, GLR_PREF_SQUARED = 2 } glr_pref_kind;
+
+typedef struct {
+  glr_loss_seqs seqs;          /* seqs even, >= 2 */
+  int32_t kind;                /* glr_pref_kind */
+  int32_t average;
+  double beta;                 /* finite, > 0 */
+  double label_smoothing;      /* in [0, 1); 0 unless SIGMOID */
+  const float* ref_logps;      /* seqs fp32: the reference's L */
+  float* loss;                 /* 1 */
+  float* logps;                /* seqs: L */
+  float* rewards;              /* seqs: beta (L - ref) */
+} glr_pref_args;
+glr_status glr_preference_loss(const glr_loss_rows* rows, const glr_pref_args* args, void* d_ws,
+                               size_t ws_bytes, void* stream);
+
+/* Clipped policy loss with a KL term.  With r = exp(lp - old) and
+ * d = ref - lp, the sum over rows of
+ *   w_t [ -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(d) - d - 1) ]
+ * with w_t = 1 / (rows trained on), or 1 / denominator, by GLR_REDUCE_TOKEN,
+ * and 1 / (seqs * rows trained on of the row's sequence) by GLR_REDUCE_SEQUENCE.
+ * The gradient of a clipped row (r A above the clipped product) is the KL
+ * term's alone.  No rows trained on: everything is 0. */
+typedef enum { GLR_REDUCE_TOKEN = 0, GLR_REDUCE_SEQUENCE = 1 } glr_reduction;
+
+typedef struct {
+  glr_loss_seqs seqs;          /* cu_seqlens and seqs: looked at where cu_seqlens is there or by SEQUENCE */
+  int32_t reduction;           /* glr_reduction */
+  double clip_low, clip_high;  /* >= 0 (infinite: no bound); clip_low <= 1 or infinite */
+  double kl_coef;              /* finite, >= 0 */
+  double denominator;          /* TOKEN: > 0, or 0 to count the rows */
+  glr_row_array old_logps;     /* fp32 */
+  glr_row_array advantages;    /* fp32 */
+  glr_row_array ref_logps;     /* fp32; needed when kl_coef > 0 */
+  float* loss;                 /* 1 */
+  float* kl;                   /* 1: sum of w_t (exp(d) - d - 1); 0 without ref_logps */
+  float* clipped;              /* 1: sum of w_t over the clipped rows */
+  float* logps;                /* batch x steps contiguous */
+} glr_policy_args;
+glr_status glr_policy_loss(const glr_loss_rows* rows, const glr_policy_args* args, void* d_ws,
+                           size_t ws_bytes, void* stream);
+
+/* Distillation from a teacher's top logits.  A row's entries k < top are the
+ * teacher's logits t_k of the tokens id_k; an entry with id_k < 0 or
+ * t_k = -inf is absent.  An index that a row repeats counts as one token with
+ * the sum of its masses.  With q the student's softmax at T (rows->temperature)
+ * and teacher masses p_k = exp(t_k / T) normalised over the entries present,
+ * or, where teacher_lse (log sum_j exp(t_j / T) over the teacher's whole
+ * vocabulary) is given, p_k = exp(t_k / T - lse) and a mass p_R = 1 - sum_k p_k
+ * (below 2^-20, or with no tokens outside the list: none) on the tokens outside,
+ *   KL  = sum_k p_k (log p_k - log q_k) + p_R (log p_R - log q_R),
+ *   row = (1 - hard_weight) T^2 KL - hard_weight log softmax(z)_y,
+ * averaged over the rows trained on (or divided by `denominator`).  A row with
+ * no entries has KL = 0. */
+typedef struct {
+  int32_t top;                 /* entries a row, in [0, 1024] */
+  int32_t id_type;             /* glr_itype */
+  int32_t teacher_type;        /* glr_dtype */
+  glr_row_array ids;           /* a row's entries are contiguous */
+  glr_row_array teacher;
+  glr_row_array teacher_lse;   /* fp32; NULL data: masses normalised over the entries */
+  double hard_weight;          /* in [0, 1]; needs targets when > 0 */
+  double denominator;          /* > 0, or 0 to count the rows */
+  float* loss;                 /* 1 */
+  float* losses;               /* batch x steps contiguous: the rows' losses before averaging */
+} glr_distill_args;
+/* vocab <= 2^19 */
+glr_status glr_distill_loss(const glr_loss_rows* rows, const glr_distill_args* args, void* d_ws,
+                            size_t ws_bytes, void* stream);
+
+/* data (count elements of dtype, contiguous) times *scale, a device scalar, in
+ * place; nothing is read or written when *scale is 1. */
+glr_status glr_loss_rescale(void* data, int64_t count, int32_t dtype, const float* scale, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* GREEDYLORE_LOSSES_H */

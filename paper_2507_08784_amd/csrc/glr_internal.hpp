@@ -4,9 +4,14 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <string>
+
 #include "greedylore.h"
 
 namespace glr {
+
+// the text glr_last_error(NULL) gives on this thread
+void set_last_error(const std::string& text);
 
 constexpr int kJB = 16;   // rows per Jacobi block
 

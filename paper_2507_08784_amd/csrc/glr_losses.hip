@@ -1,0 +1,915 @@
+// Losses over logits and their gradients: kernels and C entries of
+// include/greedylore_losses.h.
+//
+// Every loss is a function of each row's softmax: one pass finds the row's
+// maximum m and s = sum_j exp((z_j - m) / T), the row's terms follow from
+// (z_y, m, s) in fp64 by one thread, and the gradient of a row is
+// -f exp((z_j - m) / T) + g [j = y] with two scalars f, g.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+#include <string>
+#include <tuple>
+#include <utility>
+
+#include "../../include/greedylore_losses.h"
+#include "glr_internal.hpp"
+
+namespace glr {
+namespace {
+
+typedef uint16_t bf16_t;
+typedef _Float16 f16_t;
+
+constexpr int kLT = 256;                        // threads of a workgroup
+constexpr int kMaxTop = 1024;
+constexpr int64_t kMaxLossVocab = (int64_t)1 << 28;
+constexpr int64_t kMaxDistillVocab = (int64_t)1 << 19;   // the list's bitmap stays within 64 KB of LDS
+constexpr double kRestFloor = 1.0 / (1 << 20);
+constexpr double kMinTemp = 1.0 / (1 << 20);
+
+__device__ __forceinline__ float load_z(const float* p) { return *p; }
+__device__ __forceinline__ float load_z(const bf16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
+__device__ __forceinline__ float load_z(const f16_t* p) { return (float)*p; }
+__device__ __forceinline__ void store_z(float* p, float x) { *p = x; }
+__device__ __forceinline__ void store_z(bf16_t* p, float x) { *p = __builtin_bit_cast(uint16_t, (__bf16)x); }
+__device__ __forceinline__ void store_z(f16_t* p, float x) { *p = (f16_t)x; }
+
+// ---------------------------------------------------------------------------
+// arguments
+// ---------------------------------------------------------------------------
+struct RowArr {
+  const void* p;
+  int64_t sb, ss;
+};
+
+struct Rows {
+  RowArr z, dz, y;
+  int64_t ignore;
+  uint32_t rows, steps;
+  int32_t V;
+  int32_t y64;
+  float c;          // log2(e) / T: exp((z - m) / T) = 2^((z - m) c)
+  double inv_t;     // 1 / T
+  double gscale;    // grad_scale / T
+};
+
+struct Seqs {
+  const void* cu;   // NULL: the batch entries
+  int32_t n;
+  int32_t cu64;
+};
+
+__device__ __forceinline__ int64_t ld_int(const void* p, int64_t i, int w64) {
+  return w64 ? static_cast<const int64_t*>(p)[i] : (int64_t) static_cast<const int32_t*>(p)[i];
+}
+// offset i of the sequences, clamped to the rows there are
+__device__ __forceinline__ uint32_t seq_off(const Seqs& q, int64_t i, uint32_t rows) {
+  const int64_t x = ld_int(q.cu, i, q.cu64);
+  return (uint32_t)(x < 0 ? 0 : x > (int64_t)rows ? (int64_t)rows : x);
+}
+// the sequence a row belongs to, -1 if none: the last one that starts at or
+// before it (empty ones before it start there too), if it reaches that far
+__device__ __forceinline__ int seq_of(const Seqs& q, uint32_t t, uint32_t rows) {
+  int lo = 0, hi = q.n;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (seq_off(q, mid, rows) <= t) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo > 0 && t < seq_off(q, lo, rows) ? lo - 1 : -1;
+}
+
+struct RowPos {
+  uint32_t t, b, s;
+  __device__ __forceinline__ int64_t of(const RowArr& a) const { return (int64_t)b * a.sb + (int64_t)s * a.ss; }
+};
+__device__ __forceinline__ RowPos row_pos(const Rows& r, uint32_t t) {
+  RowPos p;
+  p.t = t;
+  p.b = t / r.steps;
+  p.s = t - p.b * r.steps;
+  return p;
+}
+__device__ __forceinline__ float ld_f(const RowArr& a, const RowPos& p) {
+  return static_cast<const float*>(a.p)[p.of(a)];
+}
+// the row's target: whether it is trained on, and the target (-1: outside the vocabulary)
+__device__ __forceinline__ bool row_target(const Rows& r, const RowPos& p, int& y) {
+  y = 0;
+  if (!r.y.p) return true;
+  const int64_t t = ld_int(r.y.p, p.of(r.y), r.y64);
+  y = t >= 0 && t < r.V ? (int)t : -1;
+  return t != r.ignore;
+}
+
+enum { OP_LOGP, OP_COEF, OP_POLICY };
+
+struct Terms {
+  // LOGP: logps, stats, weights; COEF: stats and coef (per row) or seq_coef (per sequence)
+  float* logps;
+  float* stats;
+  RowArr coef;
+  const float* seq_coef;
+  Seqs seqs;
+  // POLICY
+  RowArr old, adv, ref;
+  double low, high, kl;      // 1 - clip_low, 1 + clip_high, kl_coef
+  double denom;              // rows that share the mean; 0: *count
+  int by_seq;                // weight 1 / (seqs * count[sequence])
+  const int* count;
+  float* part;               // 3 x rows: w term, w kl, w clipped
+};
+
+// ---------------------------------------------------------------------------
+// workgroup reductions (all threads get the result)
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
+  return x;
+}
+template <class X>
+__device__ __forceinline__ X wave_sum(X x) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+  return x;
+}
+template <int NT>
+__device__ __forceinline__ float block_max(float x, float* sh) {
+  x = wave_max(x);
+  if constexpr (NT > 64) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = sh[0];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) x = fmaxf(x, sh[w]);
+  }
+  return x;
+}
+template <int NT, class X>
+__device__ __forceinline__ X block_sum(X x, X* sh) {
+  x = wave_sum(x);
+  if constexpr (NT > 64) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = sh[0];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) x += sh[w];
+  }
+  return x;
+}
+
+// ---------------------------------------------------------------------------
+// what a row's (z_y, m, s) give
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ double row_logp(const Rows& r, float zy, float m, float s) {
+  return ((double)zy - (double)m) * r.inv_t - log((double)s);
+}
+
+// stores the row's terms and returns g = d loss / d lp times grad_scale / T
+template <int OP>
+__device__ __forceinline__ double row_terms(const Rows& r, const Terms& a, const RowPos& p, int seq, double lp,
+                                            float m, float s) {
+  if constexpr (OP == OP_LOGP) {
+    a.logps[p.t] = (float)lp;
+    if (a.stats) {
+      a.stats[2 * (int64_t)p.t] = m;
+      a.stats[2 * (int64_t)p.t + 1] = s;
+    }
+    return a.coef.p ? (double)ld_f(a.coef, p) * r.gscale : 0.0;
+  } else if constexpr (OP == OP_COEF) {
+    return (double)(a.seq_coef ? a.seq_coef[seq] : ld_f(a.coef, p)) * r.gscale;
+  } else {
+    double w;
+    if (a.by_seq) {
+      const int n = a.count[seq];
+      w = 1.0 / ((double)a.seqs.n * (n > 0 ? n : 1));
+    } else {
+      w = 1.0 / (a.denom > 0.0 ? a.denom : (double)(*a.count > 0 ? *a.count : 1));
+    }
+    const double A = ld_f(a.adv, p);
+    const double ratio = exp(lp - (double)ld_f(a.old, p));
+    const double in = ratio < a.low ? a.low : ratio > a.high ? a.high : ratio;   // NaN stays
+    const double u = ratio * A, v = in * A;
+    const bool cut = u > v;
+    double term = cut ? -v : -u, slope = cut ? 0.0 : -u, k = 0.0;
+    if (a.ref.p) {
+      const double d = (double)ld_f(a.ref, p) - lp, x = expm1(d);
+      k = x - d;
+      term += a.kl * k;
+      slope -= a.kl * x;
+    }
+    a.logps[p.t] = (float)lp;
+    a.part[p.t] = (float)(w * term);
+    a.part[(int64_t)r.rows + p.t] = (float)(w * k);
+    a.part[2 * (int64_t)r.rows + p.t] = cut ? (float)w : 0.f;
+    return w * slope * r.gscale;
+  }
+}
+// what a masked row leaves
+template <int OP>
+__device__ __forceinline__ void row_masked(const Rows& r, const Terms& a, const RowPos& p) {
+  if constexpr (OP == OP_LOGP) {
+    a.logps[p.t] = 0.f;
+    if (a.stats) {
+      a.stats[2 * (int64_t)p.t] = 0.f;
+      a.stats[2 * (int64_t)p.t + 1] = 1.f;
+    }
+  } else if constexpr (OP == OP_POLICY) {
+    a.logps[p.t] = 0.f;
+    for (int k = 0; k < 3; ++k) a.part[k * (int64_t)r.rows + p.t] = 0.f;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// one workgroup a row
+// ---------------------------------------------------------------------------
+template <class T, int OP>
+__global__ void __launch_bounds__(kLT) k_loss_row(Rows r, Terms a) {
+  __shared__ float sh[kLT / 64];
+  __shared__ float coef[2];
+  const RowPos p = row_pos(r, blockIdx.x);
+  int y;
+  bool live = row_target(r, p, y);
+  int seq = (int)p.b;
+  if (live && a.seqs.cu) {
+    seq = seq_of(a.seqs, p.t, r.rows);
+    live = seq >= 0;
+  }
+  T* dz = r.dz.p ? static_cast<T*>(const_cast<void*>(r.dz.p)) + p.of(r.dz) : nullptr;
+  if (!live) {
+    if (threadIdx.x == 0) row_masked<OP>(r, a, p);
+    if (dz)
+      for (int j = threadIdx.x; j < r.V; j += kLT) store_z(dz + j, 0.f);
+    return;
+  }
+  const T* z = static_cast<const T*>(r.z.p) + p.of(r.z);
+  const float zy = y >= 0 ? load_z(z + y) : __builtin_nanf("");
+  float m, s;
+  if constexpr (OP == OP_COEF) {
+    m = a.stats[2 * (int64_t)p.t];
+    s = a.stats[2 * (int64_t)p.t + 1];
+  } else {
+    m = -INFINITY;
+    for (int j = threadIdx.x; j < r.V; j += kLT) m = fmaxf(m, load_z(z + j));
+    m = block_max<kLT>(m, sh);
+    s = 0.f;
+    for (int j = threadIdx.x; j < r.V; j += kLT) s += __builtin_amdgcn_exp2f((load_z(z + j) - m) * r.c);
+    s = block_sum<kLT>(s, sh);
+  }
+  if (threadIdx.x == 0) {
+    const double lp = row_logp(r, zy, m, s);
+    const double g = row_terms<OP>(r, a, p, seq, lp, m, s);
+    coef[0] = y >= 0 ? (float)(g / (double)s) : __builtin_nanf("");
+    coef[1] = (float)g;
+  }
+  if (!dz) return;
+  __syncthreads();
+  const float f = coef[0], g = coef[1];
+  for (int j = threadIdx.x; j < r.V; j += kLT) {
+    const float e = __builtin_amdgcn_exp2f((load_z(z + j) - m) * r.c);
+    store_z(dz + j, fmaf(-f, e, j == y ? g : 0.f));
+  }
+}
+
+// ---------------------------------------------------------------------------
+// distillation
+// ---------------------------------------------------------------------------
+struct Teach {
+  RowArr ids, t, lse;
+  int32_t top, id64, ttype;
+  double hard, denom;
+  const int* count;
+  float* losses;       // a row's loss
+};
+
+__device__ __forceinline__ float ld_teacher(const Teach& q, int64_t at, int k) {
+  if (q.ttype == GLR_F32) return static_cast<const float*>(q.t.p)[at + k];
+  if (q.ttype == GLR_BF16) return load_z(static_cast<const bf16_t*>(q.t.p) + at + k);
+  return load_z(static_cast<const f16_t*>(q.t.p) + at + k);
+}
+
+// One workgroup a row.  The list's tokens are marked in a bitmap over the
+// vocabulary: the mass outside the list is summed as such (the total less the
+// list's would cancel where the list holds nearly all of it), and a repeated
+// token is seen.
+template <class T>
+__global__ void __launch_bounds__(kLT) k_distill_row(Rows r, Teach q) {
+  extern __shared__ uint32_t bits[];
+  __shared__ float shf[kLT / 64];
+  __shared__ double shd[kLT / 64];
+  __shared__ int id_s[kMaxTop];
+  __shared__ float zk_s[kMaxTop], p_s[kMaxTop];
+  __shared__ int bad_s, again_s;
+  const RowPos p = row_pos(r, blockIdx.x);
+  int y;
+  const bool live = row_target(r, p, y);
+  T* dz = r.dz.p ? static_cast<T*>(const_cast<void*>(r.dz.p)) + p.of(r.dz) : nullptr;
+  if (!live) {
+    if (threadIdx.x == 0) q.losses[p.t] = 0.f;
+    if (dz)
+      for (int j = threadIdx.x; j < r.V; j += kLT) store_z(dz + j, 0.f);
+    return;
+  }
+  const T* z = static_cast<const T*>(r.z.p) + p.of(r.z);
+  for (int j = threadIdx.x; j < (r.V + 31) / 32; j += kLT) bits[j] = 0u;
+  if (threadIdx.x == 0) bad_s = again_s = 0;
+  __syncthreads();
+  const int64_t ido = p.of(q.ids), to = p.of(q.t);
+  int have = 0, distinct = 0;
+  float high = -INFINITY;
+  for (int k = threadIdx.x; k < q.top; k += kLT) {
+    const int64_t id = ld_int(q.ids.p, ido + k, q.id64);
+    const float t = ld_teacher(q, to, k);
+    int at = -1;
+    if (id >= r.V) {
+      bad_s = 1;
+    } else if (id >= 0 && t != -INFINITY) {
+      at = (int)id;
+      const uint32_t bit = 1u << (at & 31);
+      if (atomicOr(&bits[at >> 5], bit) & bit) again_s = 1;
+      else ++distinct;
+      ++have;
+      high = fmaxf(high, t);
+    }
+    id_s[k] = at;
+    p_s[k] = t;
+    zk_s[k] = at >= 0 ? load_z(z + at) : 0.f;
+  }
+  have = block_sum<kLT, int>(have, reinterpret_cast<int*>(shf));
+  distinct = block_sum<kLT, int>(distinct, reinterpret_cast<int*>(shf));
+  high = block_max<kLT>(high, shf);
+  const bool rest = q.lse.p != nullptr && have > 0 && distinct < r.V;
+  const bool two = q.hard > 0.0 && r.inv_t != 1.0;
+  const float c1 = 1.44269504088896340736f;
+
+  float m = -INFINITY;
+  for (int j = threadIdx.x; j < r.V; j += kLT) m = fmaxf(m, load_z(z + j));
+  m = block_max<kLT>(m, shf);
+  float s = 0.f, so = 0.f, s1 = 0.f;
+  for (int j = threadIdx.x; j < r.V; j += kLT) {
+    const float d = load_z(z + j) - m, e = __builtin_amdgcn_exp2f(d * r.c);
+    s += e;
+    if (rest && !(bits[j >> 5] >> (j & 31) & 1u)) so += e;
+    if (two) s1 += __builtin_amdgcn_exp2f(d * c1);
+  }
+  s = block_sum<kLT>(s, shf);
+  if (rest) so = block_sum<kLT>(so, shf);
+  s1 = two ? block_sum<kLT>(s1, shf) : s;
+
+  // the teacher's masses and their divergence
+  const double logs = log((double)s);
+  double norm;
+  if (q.lse.p) {
+    norm = ld_f(q.lse, p);
+  } else {
+    double sum = 0.0;
+    for (int k = threadIdx.x; k < q.top; k += kLT)
+      if (id_s[k] >= 0) sum += exp(((double)p_s[k] - (double)high) * r.inv_t);
+    norm = (double)high * r.inv_t + log(block_sum<kLT, double>(sum, shd));
+  }
+  double kl = 0.0, mass = 0.0;
+  for (int k = threadIdx.x; k < q.top; k += kLT) {
+    double pk = 0.0;
+    if (id_s[k] >= 0) {
+      const double lpk = (double)p_s[k] * r.inv_t - norm;
+      pk = exp(lpk);
+      if (pk > 0.0) kl += pk * (lpk - (((double)zk_s[k] - (double)m) * r.inv_t - logs));
+      else kl += pk;        // (NaN stays)
+    }
+    p_s[k] = (float)pk;
+    mass += pk;
+  }
+  kl = block_sum<kLT, double>(kl, shd);
+  mass = block_sum<kLT, double>(mass, shd);
+  double left = 0.0;
+  if (rest) {
+    left = 1.0 - mass;
+    if (left < kRestFloor) left = 0.0;
+    if (left != 0.0) kl += left * (log(left) - (log((double)so) - logs));
+  }
+  double row = (1.0 - q.hard) * kl / (r.inv_t * r.inv_t);
+  const float nan = __builtin_nanf("");
+  if (q.hard > 0.0) {
+    const float zy = y >= 0 ? load_z(z + y) : nan;
+    row -= q.hard * ((double)zy - (double)m - log((double)s1));
+  }
+  const bool bad = bad_s != 0 || y < 0;
+  if (threadIdx.x == 0) q.losses[p.t] = bad ? nan : (float)row;
+  if (!dz) return;
+  const double n = q.denom > 0.0 ? q.denom : (double)(q.count ? (*q.count > 0 ? *q.count : 1) : r.rows);
+  const double scale = r.gscale / r.inv_t / n;     // grad_scale / n
+  const double soft = (1.0 - q.hard) / r.inv_t * scale;
+  const float f_out = bad ? nan : (float)(soft * ((mass + left) / (double)s - (left != 0.0 ? left / (double)so : 0.0)));
+  const float f_in = (float)(soft * (mass + left) / (double)s);
+  const float f1 = (float)(q.hard * scale / (double)s1), h = (float)(q.hard * scale), sf = (float)soft;
+  for (int j = threadIdx.x; j < r.V; j += kLT) {
+    const float d = load_z(z + j) - m;
+    float x = f_out * __builtin_amdgcn_exp2f(d * r.c);
+    if (q.hard > 0.0) {
+      x = fmaf(f1, __builtin_amdgcn_exp2f(d * c1), x);
+      if (j == y) x -= h;
+    }
+    if (bits[j >> 5] >> (j & 31) & 1u) continue;
+    store_z(dz + j, x);
+  }
+  for (int k = threadIdx.x; k < q.top; k += kLT) {
+    const int j = id_s[k];
+    if (j < 0) continue;
+    float mine = p_s[k];
+    if (again_s) {             // a repeated token: its first entry has the sum of its masses
+      bool first = true;
+      for (int i = 0; i < k; ++i) first = first && id_s[i] != j;
+      if (!first) continue;
+      for (int i = k + 1; i < q.top; ++i)
+        if (id_s[i] == j) mine += p_s[i];
+    }
+    const float d = zk_s[k] - m;
+    float x = fmaf(f_in, __builtin_amdgcn_exp2f(d * r.c), -sf * mine);
+    if (q.hard > 0.0) {
+      x = fmaf(f1, __builtin_amdgcn_exp2f(d * c1), x);
+      if (j == y) x -= h;
+    }
+    store_z(dz + j, bad ? nan : x);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// counts, pairs and totals
+// ---------------------------------------------------------------------------
+// rows trained on: of everything (one workgroup) or of each sequence
+__global__ void __launch_bounds__(1024) k_loss_count(Rows r, Seqs q, int by_seq, int* count) {
+  __shared__ int sh[16];
+  uint32_t lo = 0, hi = r.rows;
+  if (by_seq) {
+    lo = q.cu ? seq_off(q, blockIdx.x, r.rows) : blockIdx.x * r.steps;
+    hi = q.cu ? seq_off(q, (int64_t)blockIdx.x + 1, r.rows) : lo + r.steps;
+  } else if (q.cu) {
+    lo = seq_off(q, 0, r.rows);
+    hi = seq_off(q, q.n, r.rows);
+  }
+  int n = 0;
+  for (uint64_t t = (uint64_t)lo + threadIdx.x; t < hi; t += 1024) {
+    int y;
+    n += row_target(r, row_pos(r, (uint32_t)t), y);
+  }
+  n = block_sum<1024>(n, sh);
+  if (threadIdx.x == 0) count[blockIdx.x] = n;
+}
+
+struct Pairs {
+  Seqs seqs;
+  int kind, average;
+  double beta, smooth;
+  const float* ref;
+  const float* lp;     // of the rows
+  float* logps;
+  float* rewards;
+  float* coef;         // d loss / d lp of a sequence's rows
+  float* part;         // a pair's loss
+};
+
+__global__ void __launch_bounds__(kLT) k_loss_pairs(Rows r, Pairs q) {
+  __shared__ double shd[kLT / 64];
+  __shared__ int shi[kLT / 64];
+  const int half = q.seqs.n >> 1;
+  double L[2];
+  int n[2];
+  for (int side = 0; side < 2; ++side) {
+    const int i = (int)blockIdx.x + side * half;
+    const uint32_t lo = q.seqs.cu ? seq_off(q.seqs, i, r.rows) : (uint32_t)i * r.steps;
+    const uint32_t hi = q.seqs.cu ? seq_off(q.seqs, i + 1, r.rows) : lo + r.steps;
+    double x = 0.0;
+    int c = 0;
+    for (uint64_t t = (uint64_t)lo + threadIdx.x; t < hi; t += kLT) {
+      int y;
+      if (row_target(r, row_pos(r, (uint32_t)t), y)) {
+        x += q.lp[t];
+        ++c;
+      }
+    }
+    L[side] = block_sum<kLT, double>(x, shd);
+    n[side] = q.average ? block_sum<kLT, int>(c, shi) : 1;
+    if (n[side] < 1) n[side] = 1;
+    L[side] /= n[side];
+  }
+  if (threadIdx.x) return;
+  const int i = blockIdx.x, j = i + half;
+  const double rc = L[0] - (double)q.ref[i], rr = L[1] - (double)q.ref[j];
+  const double delta = rc - rr, h = q.beta * delta;
+  double loss, slope;
+  if (q.kind == GLR_PREF_SIGMOID) {
+    const double soft = log1p(exp(-fabs(h)));
+    const double neg = soft + (h < 0.0 ? -h : 0.0), pos = soft + (h > 0.0 ? h : 0.0);   // -log sigma(h), -log sigma(-h)
+    loss = (1.0 - q.smooth) * neg + q.smooth * pos;
+    slope = q.beta * (q.smooth - 1.0 / (1.0 + exp(h)));
+    if (h != h) loss = h;
+  } else if (q.kind == GLR_PREF_HINGE) {
+    loss = h < 1.0 ? 1.0 - h : h == h ? 0.0 : h;
+    slope = h < 1.0 ? -q.beta : h == h ? 0.0 : h;
+  } else {
+    const double off = delta - 0.5 / q.beta;
+    loss = off * off;
+    slope = 2.0 * off;
+  }
+  q.logps[i] = (float)L[0];
+  q.logps[j] = (float)L[1];
+  q.rewards[i] = (float)(q.beta * rc);
+  q.rewards[j] = (float)(q.beta * rr);
+  q.part[i] = (float)loss;
+  if (q.coef) {
+    q.coef[i] = (float)(slope / half / n[0]);
+    q.coef[j] = (float)(-slope / half / n[1]);
+  }
+}
+
+// out[k] = scale sum_i part[k][i]; by denom (0: *count, else 1) if there is one
+__global__ void __launch_bounds__(1024) k_loss_total(const float* part, int64_t n, double denom, const int* count,
+                                                    float* o0, float* o1, float* o2) {
+  __shared__ double sh[16];
+  float* out = blockIdx.x == 0 ? o0 : blockIdx.x == 1 ? o1 : o2;
+  double x = 0.0;
+  for (int64_t i = threadIdx.x; i < n; i += 1024) x += part[blockIdx.x * n + i];
+  x = block_sum<1024, double>(x, sh);
+  if (threadIdx.x == 0) *out = (float)(x / (denom > 0.0 ? denom : (double)(*count > 0 ? *count : 1)));
+}
+
+template <class T>
+__global__ void __launch_bounds__(kLT) k_loss_rescale(T* x, int64_t n, const float* scale) {
+  const float f = *scale;
+  if (f == 1.f) return;
+  for (int64_t i = (int64_t)blockIdx.x * kLT + threadIdx.x; i < n; i += (int64_t)gridDim.x * kLT)
+    store_z(x + i, load_z(x + i) * f);
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+struct Refusal {
+  glr_status s;
+  std::string why;
+};
+
+[[noreturn]] void refuse(glr_status s, const char* f, ...) {
+  char buf[256];
+  va_list ap;
+  va_start(ap, f);
+  vsnprintf(buf, sizeof buf, f, ap);
+  va_end(ap);
+  throw Refusal{s, buf};
+}
+
+// a C entry: nothing is thrown across it
+template <class F>
+glr_status entry(F&& body) {
+  try {
+    body();
+    return GLR_OK;
+  } catch (const Refusal& x) {
+    try {
+      set_last_error(x.why);
+    } catch (...) {
+    }
+    return x.s;
+  } catch (...) {
+    return GLR_ERR_DEVICE;
+  }
+}
+
+template <class... P, class... A>
+void launch(const char* what, void (*k)(P...), unsigned grid, unsigned block, size_t lds, void* stream, A&&... a) {
+  if (!grid) return;
+  std::tuple<P...> t(std::forward<A>(a)...);
+  std::apply(
+      [&](P&... x) {
+        void* args[] = {(void*)&x...};
+        const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(k), dim3(grid), dim3(block), args, lds,
+                                             static_cast<hipStream_t>(stream));
+        if (e != hipSuccess) {
+          (void)hipGetLastError();
+          refuse(GLR_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
+        }
+      },
+      t);
+}
+
+RowArr arr(const glr_row_array& a) { return RowArr{a.data, a.stride_b, a.stride_s}; }
+
+void check_array(const glr_row_array& a, size_t align, const char* name) {
+  if (!a.data) refuse(GLR_ERR_INVALID_ARG, "%s is NULL", name);
+  if (reinterpret_cast<uintptr_t>(a.data) % align)
+    refuse(GLR_ERR_INVALID_ARG, "%s is not aligned to its elements", name);
+}
+void check_out(const void* p, const char* name) {
+  if (!p) refuse(GLR_ERR_INVALID_ARG, "%s is NULL", name);
+  if (reinterpret_cast<uintptr_t>(p) % 4) refuse(GLR_ERR_INVALID_ARG, "%s is not aligned to its elements", name);
+}
+
+void check_dims(const glr_loss_rows* x) {
+  if (!x) refuse(GLR_ERR_INVALID_ARG, "rows is NULL");
+  constexpr int64_t lim = (int64_t)1 << 31;
+  if (x->batch < 0 || x->steps < 0 || x->batch >= lim || x->steps >= lim || x->batch * x->steps >= lim)
+    refuse(GLR_ERR_SHAPE, "batch %lld x steps %lld: rows must be in [0, 2^31)", (long long)x->batch, (long long)x->steps);
+  if (x->vocab < 1 || x->vocab > kMaxLossVocab)
+    refuse(GLR_ERR_SHAPE, "vocab %lld must be in [1, 2^28]", (long long)x->vocab);
+  if (x->dtype < GLR_F32 || x->dtype > GLR_F16) refuse(GLR_ERR_INVALID_ARG, "unknown logits type");
+}
+
+Rows check_rows(const glr_loss_rows* x, bool need_targets) {
+  check_dims(x);
+  if (x->target_type != GLR_I32 && x->target_type != GLR_I64) refuse(GLR_ERR_INVALID_ARG, "unknown target type");
+  if (!(x->temperature >= kMinTemp && x->temperature <= 1.0 / kMinTemp))
+    refuse(GLR_ERR_INVALID_ARG, "temperature must be in [2^-20, 2^20]");
+  if (!std::isfinite(x->grad_scale)) refuse(GLR_ERR_INVALID_ARG, "grad_scale must be finite");
+  const size_t es = x->dtype == GLR_F32 ? 4 : 2;
+  if (x->batch * x->steps > 0) {
+    check_array(x->logits, es, "logits");
+    if (x->dlogits.data) check_array(x->dlogits, es, "dlogits");
+    if (need_targets) check_array(x->targets, x->target_type == GLR_I64 ? 8 : 4, "targets");
+  }
+  Rows r;
+  r.z = arr(x->logits);
+  r.dz = arr(x->dlogits);
+  r.y = arr(x->targets);
+  r.ignore = x->ignore_index;
+  r.rows = (uint32_t)(x->batch * x->steps);
+  r.steps = (uint32_t)(x->steps > 0 ? x->steps : 1);
+  r.V = (int32_t)x->vocab;
+  r.y64 = x->target_type == GLR_I64;
+  r.inv_t = 1.0 / x->temperature;
+  r.c = (float)(1.44269504088896340736 * r.inv_t);
+  r.gscale = x->grad_scale * r.inv_t;
+  return r;
+}
+
+Seqs check_seqs(const glr_loss_rows* x, const glr_loss_seqs& q) {
+  if (q.seqs < 1 || q.seqs >= ((int64_t)1 << 31) - 1) refuse(GLR_ERR_SHAPE, "seqs must be in [1, 2^31 - 2]");
+  if (!q.cu_seqlens) {
+    if (q.seqs != x->batch) refuse(GLR_ERR_INVALID_ARG, "seqs must be batch where cu_seqlens is NULL");
+  } else {
+    if (q.cu_type != GLR_I32 && q.cu_type != GLR_I64) refuse(GLR_ERR_INVALID_ARG, "unknown cu_seqlens type");
+    if (reinterpret_cast<uintptr_t>(q.cu_seqlens) % (q.cu_type == GLR_I64 ? 8 : 4))
+      refuse(GLR_ERR_INVALID_ARG, "cu_seqlens is not aligned to its elements");
+  }
+  return Seqs{q.cu_seqlens, (int32_t)q.seqs, q.cu_type == GLR_I64};
+}
+
+constexpr size_t up16(size_t x) { return (x + 15) / 16 * 16; }
+
+// scratch of a call, in 16-byte aligned pieces
+struct Scratch {
+  size_t lp = 0, stats = 0, coef = 0, part = 0, count = 0, bytes = 0;
+  size_t take(size_t n) {
+    const size_t at = bytes;
+    bytes += up16(n);
+    return at;
+  }
+};
+Scratch scratch_of(int op, int64_t rows, int64_t seqs, bool grad) {
+  Scratch s;
+  if (op == GLR_LOSS_PREFERENCE) {
+    s.lp = s.take(4 * rows);
+    s.stats = s.take(grad ? 8 * rows : 0);
+    s.coef = s.take(4 * seqs);
+    s.part = s.take(2 * seqs);
+  } else if (op == GLR_LOSS_POLICY) {
+    s.part = s.take(12 * rows);
+    s.count = s.take(4 * (seqs > 1 ? seqs : 1));
+  } else if (op == GLR_LOSS_DISTILL) {
+    s.count = s.take(4);
+  }
+  return s;
+}
+char* check_ws(const Scratch& s, void* ws, size_t bytes) {
+  if (s.bytes > bytes)
+    refuse(GLR_ERR_BUFFER_TOO_SMALL, "workspace of %zu bytes, %zu needed", bytes, s.bytes);
+  if (s.bytes && !ws) refuse(GLR_ERR_INVALID_ARG, "workspace is NULL");
+  if (reinterpret_cast<uintptr_t>(ws) % 16) refuse(GLR_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+  return static_cast<char*>(ws);
+}
+
+template <int OP>
+void run_rows(int dtype, const Rows& r, const Terms& a, void* stream) {
+  auto* k = dtype == GLR_F32 ? k_loss_row<float, OP> : dtype == GLR_BF16 ? k_loss_row<bf16_t, OP> : k_loss_row<f16_t, OP>;
+  launch("loss rows", k, r.rows, kLT, 0, stream, r, a);
+}
+
+}  // namespace
+}  // namespace glr
+
+using namespace glr;
+
+extern "C" {
+
+glr_status glr_loss_workspace_bytes(const glr_loss_rows* rows, int32_t op, int64_t seqs, size_t* bytes) {
+  return entry([&] {
+    check_dims(rows);
+    if (!bytes) refuse(GLR_ERR_INVALID_ARG, "bytes is NULL");
+    if (op < GLR_LOSS_LOGPROBS || op > GLR_LOSS_DISTILL) refuse(GLR_ERR_INVALID_ARG, "unknown op");
+    if (seqs < 0 || seqs >= ((int64_t)1 << 31) - 1) refuse(GLR_ERR_SHAPE, "seqs must be in [0, 2^31 - 2]");
+    *bytes = scratch_of(op, rows->batch * rows->steps, seqs, rows->dlogits.data != nullptr).bytes;
+  });
+}
+
+glr_status glr_token_logprobs(const glr_loss_rows* rows, const glr_row_array* weights, float* logps, float* stats,
+                              void* d_ws, size_t ws_bytes, void* stream) {
+  return entry([&] {
+    const Rows r = check_rows(rows, true);
+    check_ws(scratch_of(GLR_LOSS_LOGPROBS, r.rows, 0, r.dz.p != nullptr), d_ws, ws_bytes);
+    if (!r.rows) return;
+    check_out(logps, "logps");
+    if (stats) check_out(stats, "stats");
+    if (r.dz.p) {
+      if (!weights) refuse(GLR_ERR_INVALID_ARG, "a gradient needs weights");
+      check_array(*weights, 4, "weights");
+    }
+    Terms a = {};
+    a.logps = logps;
+    a.stats = stats;
+    if (r.dz.p) a.coef = arr(*weights);
+    run_rows<OP_LOGP>(rows->dtype, r, a, stream);
+  });
+}
+
+glr_status glr_token_logprobs_backward(const glr_loss_rows* rows, const float* stats, const glr_row_array* grad_logps,
+                                       void* stream) {
+  return entry([&] {
+    const Rows r = check_rows(rows, true);
+    if (!r.rows) return;
+    if (!r.dz.p) refuse(GLR_ERR_INVALID_ARG, "dlogits is NULL");
+    check_out(stats, "stats");
+    if (!grad_logps) refuse(GLR_ERR_INVALID_ARG, "grad_logps is NULL");
+    check_array(*grad_logps, 4, "grad_logps");
+    Terms a = {};
+    a.stats = const_cast<float*>(stats);
+    a.coef = arr(*grad_logps);
+    run_rows<OP_COEF>(rows->dtype, r, a, stream);
+  });
+}
+
+glr_status glr_preference_loss(const glr_loss_rows* rows, const glr_pref_args* x, void* d_ws, size_t ws_bytes,
+                               void* stream) {
+  return entry([&] {
+    const Rows r = check_rows(rows, true);
+    if (!x) refuse(GLR_ERR_INVALID_ARG, "args is NULL");
+    const Seqs q = check_seqs(rows, x->seqs);
+    if (q.n < 2 || q.n % 2) refuse(GLR_ERR_SHAPE, "seqs must be even and at least 2");
+    if (x->kind < GLR_PREF_SIGMOID || x->kind > GLR_PREF_SQUARED) refuse(GLR_ERR_INVALID_ARG, "unknown kind");
+    if (!(std::isfinite(x->beta) && x->beta > 0.0)) refuse(GLR_ERR_INVALID_ARG, "beta must be finite and > 0");
+    if (!(x->label_smoothing >= 0.0 && x->label_smoothing < 1.0))
+      refuse(GLR_ERR_INVALID_ARG, "label_smoothing must be in [0, 1)");
+    if (x->label_smoothing != 0.0 && x->kind != GLR_PREF_SIGMOID)
+      refuse(GLR_ERR_INVALID_ARG, "label_smoothing applies to the sigmoid loss only");
+    check_out(x->ref_logps, "ref_logps");
+    check_out(x->loss, "loss");
+    check_out(x->logps, "logps");
+    check_out(x->rewards, "rewards");
+    const Scratch s = scratch_of(GLR_LOSS_PREFERENCE, r.rows, q.n, r.dz.p != nullptr);
+    char* ws = check_ws(s, d_ws, ws_bytes);
+    Terms a = {};
+    a.seqs = q;
+    a.logps = reinterpret_cast<float*>(ws + s.lp);
+    a.stats = r.dz.p ? reinterpret_cast<float*>(ws + s.stats) : nullptr;
+    Rows f = r;
+    f.dz.p = nullptr;
+    run_rows<OP_LOGP>(rows->dtype, f, a, stream);
+    Pairs b = {};
+    b.seqs = q;
+    b.kind = x->kind;
+    b.average = x->average;
+    b.beta = x->beta;
+    b.smooth = x->label_smoothing;
+    b.ref = x->ref_logps;
+    b.lp = a.logps;
+    b.logps = x->logps;
+    b.rewards = x->rewards;
+    b.coef = reinterpret_cast<float*>(ws + s.coef);
+    b.part = reinterpret_cast<float*>(ws + s.part);
+    launch("loss pairs", k_loss_pairs, q.n / 2, kLT, 0, stream, r, b);
+    launch("loss total", k_loss_total, 1, 1024, 0, stream, b.part, (int64_t)(q.n / 2), (double)(q.n / 2), nullptr,
+           x->loss, nullptr, nullptr);
+    if (r.dz.p) {
+      a.seq_coef = b.coef;
+      run_rows<OP_COEF>(rows->dtype, r, a, stream);
+    }
+  });
+}
+
+glr_status glr_policy_loss(const glr_loss_rows* rows, const glr_policy_args* x, void* d_ws, size_t ws_bytes,
+                           void* stream) {
+  return entry([&] {
+    const Rows r = check_rows(rows, true);
+    if (!x) refuse(GLR_ERR_INVALID_ARG, "args is NULL");
+    if (x->reduction != GLR_REDUCE_TOKEN && x->reduction != GLR_REDUCE_SEQUENCE)
+      refuse(GLR_ERR_INVALID_ARG, "unknown reduction");
+    const bool by_seq = x->reduction == GLR_REDUCE_SEQUENCE;
+    Seqs q = {};
+    if (by_seq || x->seqs.cu_seqlens) q = check_seqs(rows, x->seqs);
+    if (!(x->clip_low >= 0.0 && (x->clip_low <= 1.0 || std::isinf(x->clip_low))))
+      refuse(GLR_ERR_INVALID_ARG, "clip_low must be in [0, 1], or infinite");
+    if (!(x->clip_high >= 0.0)) refuse(GLR_ERR_INVALID_ARG, "clip_high must be >= 0");
+    if (!(std::isfinite(x->kl_coef) && x->kl_coef >= 0.0)) refuse(GLR_ERR_INVALID_ARG, "kl_coef must be finite and >= 0");
+    if (!(std::isfinite(x->denominator) && x->denominator >= 0.0))
+      refuse(GLR_ERR_INVALID_ARG, "denominator must be finite and > 0 (0: the rows trained on)");
+    if (by_seq && x->denominator != 0.0)
+      refuse(GLR_ERR_INVALID_ARG, "denominator applies to the token reduction only");
+    if (x->kl_coef > 0.0 && !x->ref_logps.data) refuse(GLR_ERR_INVALID_ARG, "kl_coef > 0 needs ref_logps");
+    check_out(x->loss, "loss");
+    check_out(x->kl, "kl");
+    check_out(x->clipped, "clipped");
+    if (r.rows) {
+      check_array(x->old_logps, 4, "old_logps");
+      check_array(x->advantages, 4, "advantages");
+      if (x->ref_logps.data) check_array(x->ref_logps, 4, "ref_logps");
+      check_out(x->logps, "logps");
+    }
+    const Scratch s = scratch_of(GLR_LOSS_POLICY, r.rows, by_seq ? q.n : 0, r.dz.p != nullptr);
+    char* ws = check_ws(s, d_ws, ws_bytes);
+    Terms a = {};
+    a.seqs = q;
+    a.logps = x->logps;
+    a.old = arr(x->old_logps);
+    a.adv = arr(x->advantages);
+    a.ref = arr(x->ref_logps);
+    a.low = 1.0 - x->clip_low;
+    a.high = 1.0 + x->clip_high;
+    a.kl = x->kl_coef;
+    a.denom = x->denominator;
+    a.by_seq = by_seq;
+    int* count = reinterpret_cast<int*>(ws + s.count);
+    a.count = count;
+    a.part = reinterpret_cast<float*>(ws + s.part);
+    if (by_seq || a.denom == 0.0) launch("loss count", k_loss_count, by_seq ? q.n : 1, 1024, 0, stream, r, q, (int)by_seq, count);
+    run_rows<OP_POLICY>(rows->dtype, r, a, stream);
+    launch("loss total", k_loss_total, 3, 1024, 0, stream, a.part, (int64_t)r.rows, 1.0, nullptr, x->loss, x->kl,
+           x->clipped);
+  });
+}
+
+glr_status glr_distill_loss(const glr_loss_rows* rows, const glr_distill_args* x, void* d_ws, size_t ws_bytes,
+                            void* stream) {
+  return entry([&] {
+    const Rows r = check_rows(rows, rows && rows->targets.data != nullptr);
+    if (!x) refuse(GLR_ERR_INVALID_ARG, "args is NULL");
+    if (r.V > kMaxDistillVocab) refuse(GLR_ERR_SHAPE, "vocab %d above 2^19", r.V);
+    if (x->top < 0 || x->top > kMaxTop) refuse(GLR_ERR_SHAPE, "top must be in [0, %d]", kMaxTop);
+    if (x->id_type != GLR_I32 && x->id_type != GLR_I64) refuse(GLR_ERR_INVALID_ARG, "unknown index type");
+    if (x->teacher_type < GLR_F32 || x->teacher_type > GLR_F16) refuse(GLR_ERR_INVALID_ARG, "unknown teacher type");
+    if (!(x->hard_weight >= 0.0 && x->hard_weight <= 1.0)) refuse(GLR_ERR_INVALID_ARG, "hard_weight must be in [0, 1]");
+    if (x->hard_weight > 0.0 && !r.y.p) refuse(GLR_ERR_INVALID_ARG, "hard_weight > 0 needs targets");
+    if (!(std::isfinite(x->denominator) && x->denominator >= 0.0))
+      refuse(GLR_ERR_INVALID_ARG, "denominator must be finite and > 0 (0: the rows trained on)");
+    check_out(x->loss, "loss");
+    if (r.rows) {
+      if (x->top) {
+        check_array(x->ids, x->id_type == GLR_I64 ? 8 : 4, "ids");
+        check_array(x->teacher, x->teacher_type == GLR_F32 ? 4 : 2, "teacher");
+      }
+      if (x->teacher_lse.data) check_array(x->teacher_lse, 4, "teacher_lse");
+      check_out(x->losses, "losses");
+    }
+    const Scratch s = scratch_of(GLR_LOSS_DISTILL, r.rows, 0, r.dz.p != nullptr);
+    char* ws = check_ws(s, d_ws, ws_bytes);
+    int* count = reinterpret_cast<int*>(ws + s.count);
+    const bool counted = x->denominator == 0.0 && r.y.p;
+    Teach q = {};
+    q.ids = arr(x->ids);
+    q.t = arr(x->teacher);
+    q.lse = arr(x->teacher_lse);
+    q.top = x->top;
+    q.id64 = x->id_type == GLR_I64;
+    q.ttype = x->teacher_type;
+    q.hard = x->hard_weight;
+    q.denom = x->denominator;
+    q.count = counted ? count : nullptr;
+    q.losses = x->losses;
+    if (counted) launch("loss count", k_loss_count, 1, 1024, 0, stream, r, Seqs{}, 0, count);
+    auto* k = rows->dtype == GLR_F32 ? k_distill_row<float> : rows->dtype == GLR_BF16 ? k_distill_row<bf16_t> : k_distill_row<f16_t>;
+    launch("distillation rows", k, r.rows, kLT, ((size_t)r.V + 31) / 32 * 4, stream, r, q);
+    const double denom = counted ? 0.0 : q.denom > 0.0 ? q.denom : r.rows ? (double)r.rows : 1.0;
+    launch("loss total", k_loss_total, 1, 1024, 0, stream, x->losses, (int64_t)r.rows, denom, count, x->loss, nullptr,
+           nullptr);
+  });
+}
+
+glr_status glr_loss_rescale(void* data, int64_t count, int32_t dtype, const float* scale, void* stream) {
+  return entry([&] {
+    if (dtype < GLR_F32 || dtype > GLR_F16) refuse(GLR_ERR_INVALID_ARG, "unknown type");
+    if (count < 0) refuse(GLR_ERR_SHAPE, "count must be >= 0");
+    if (!count) return;
+    check_array(glr_row_array{data, 0, 0}, dtype == GLR_F32 ? 4 : 2, "data");
+    check_out(scale, "scale");
+    const int64_t want = (count + kLT - 1) / kLT;
+    const unsigned grid = (unsigned)(want < 4096 ? want : 4096);
+    if (dtype == GLR_F32) launch("rescale", k_loss_rescale<float>, grid, kLT, 0, stream, static_cast<float*>(data), count, scale);
+    else if (dtype == GLR_BF16) launch("rescale", k_loss_rescale<bf16_t>, grid, kLT, 0, stream, static_cast<bf16_t*>(data), count, scale);
+    else launch("rescale", k_loss_rescale<f16_t>, grid, kLT, 0, stream, static_cast<f16_t*>(data), count, scale);
+  });
+}
+
+}  // extern "C"

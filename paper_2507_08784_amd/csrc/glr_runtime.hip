@@ -32,7 +32,7 @@ constexpr int kMaxLanes = 4;            // streams the matrices of one step are 
 
 inline uint64_t align_up(uint64_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
-thread_local std::string g_create_error;
+thread_local std::string g_create_error;   // text of the last failed call without a handle
 
 struct WsLayout {
   uint64_t off_Mbar, off_Q, off_Qpart, off_Qf, off_Qe, off_Pf, off_Pe, off_lam, off_amax, off_umax, off_W, off_Utw, off_gram, off_gram2, off_V, off_V64, off_gpart, off_skip,
@@ -1157,6 +1157,10 @@ void release_lanes(glr_handle* h) {
 }
 
 }  // namespace
+
+namespace glr {
+void set_last_error(const std::string& text) { g_create_error = text; }
+}  // namespace glr
 
 extern "C" {
 
