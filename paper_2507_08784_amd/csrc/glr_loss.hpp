@@ -1,0 +1,347 @@
+// Shared by the loss kernels (glr_losses.hip, glr_loss_rows.hip,
+// glr_distill.hip): arguments, element access, workgroup reductions, and the
+// row in registers.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <cstdarg>
+#include <cstdio>
+#include <string>
+#include <tuple>
+#include <utility>
+
+#include "../../include/greedylore_losses.h"
+#include "glr_internal.hpp"
+
+namespace glr {
+
+typedef uint16_t bf16_t;
+typedef _Float16 f16_t;
+
+constexpr int kLT = 256;                        // threads of the small kernels
+constexpr int kMaxTop = 1024;
+constexpr int64_t kMaxLossVocab = (int64_t)1 << 28;
+constexpr int64_t kMaxDistillVocab = (int64_t)1 << 19;   // the list's bitmap stays within 64 KB of LDS
+constexpr double kRestFloor = 1.0 / (1 << 20);
+constexpr double kMinTemp = 1.0 / (1 << 20);
+
+__device__ __forceinline__ float load_z(const float* p) { return *p; }
+__device__ __forceinline__ float load_z(const bf16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
+__device__ __forceinline__ float load_z(const f16_t* p) { return (float)*p; }
+__device__ __forceinline__ void store_z(float* p, float x) { *p = x; }
+__device__ __forceinline__ void store_z(bf16_t* p, float x) { *p = __builtin_bit_cast(uint16_t, (__bf16)x); }
+__device__ __forceinline__ void store_z(f16_t* p, float x) { *p = (f16_t)x; }
+
+// ---------------------------------------------------------------------------
+// arguments
+// ---------------------------------------------------------------------------
+struct RowArr {
+  const void* p;
+  int64_t sb, ss;
+};
+
+struct Rows {
+  RowArr z, dz, y;
+  int64_t ignore;
+  uint32_t rows, steps;
+  int32_t V;
+  int32_t y64;
+  float c;          // log2(e) / T: exp((z - m) / T) = 2^((z - m) c)
+  double inv_t;     // 1 / T
+  double gscale;    // grad_scale / T
+};
+
+struct Seqs {
+  const void* cu;   // NULL: the batch entries
+  int32_t n;
+  int32_t cu64;
+};
+
+__device__ __forceinline__ int64_t ld_int(const void* p, int64_t i, int w64) {
+  return w64 ? static_cast<const int64_t*>(p)[i] : (int64_t) static_cast<const int32_t*>(p)[i];
+}
+// offset i of the sequences, clamped to the rows there are
+__device__ __forceinline__ uint32_t seq_off(const Seqs& q, int64_t i, uint32_t rows) {
+  const int64_t x = ld_int(q.cu, i, q.cu64);
+  return (uint32_t)(x < 0 ? 0 : x > (int64_t)rows ? (int64_t)rows : x);
+}
+// the sequence a row belongs to, -1 if none: the last one that starts at or
+// before it (empty ones before it start there too), if it reaches that far
+__device__ __forceinline__ int seq_of(const Seqs& q, uint32_t t, uint32_t rows) {
+  int lo = 0, hi = q.n;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (seq_off(q, mid, rows) <= t) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo > 0 && t < seq_off(q, lo, rows) ? lo - 1 : -1;
+}
+
+struct RowPos {
+  uint32_t t, b, s;
+  __device__ __forceinline__ int64_t of(const RowArr& a) const { return (int64_t)b * a.sb + (int64_t)s * a.ss; }
+};
+__device__ __forceinline__ RowPos row_pos(const Rows& r, uint32_t t) {
+  RowPos p;
+  p.t = t;
+  p.b = t / r.steps;
+  p.s = t - p.b * r.steps;
+  return p;
+}
+__device__ __forceinline__ float ld_f(const RowArr& a, const RowPos& p) {
+  return static_cast<const float*>(a.p)[p.of(a)];
+}
+// the row's target: whether it is trained on, and the target (-1: outside the vocabulary)
+__device__ __forceinline__ bool row_target(const Rows& r, const RowPos& p, int& y) {
+  y = 0;
+  if (!r.y.p) return true;
+  const int64_t t = ld_int(r.y.p, p.of(r.y), r.y64);
+  y = t >= 0 && t < r.V ? (int)t : -1;
+  return t != r.ignore;
+}
+
+enum { OP_LOGP, OP_POLICY, OP_COEF };
+
+struct Terms {
+  int32_t op;
+  // LOGP: logps, stats, weights; COEF: stats and coef (per row) or seq_coef (per sequence)
+  float* logps;
+  float* stats;
+  RowArr coef;
+  const float* seq_coef;
+  Seqs seqs;
+  // POLICY
+  RowArr old, adv, ref;
+  double low, high, kl;      // 1 - clip_low, 1 + clip_high, kl_coef
+  double denom;              // rows that share the mean; 0: *count
+  int by_seq;                // weight 1 / (seqs * count[sequence])
+  const int* count;
+  float* part;               // 3 x rows: w term, w kl, w clipped
+};
+
+// ---------------------------------------------------------------------------
+// workgroup reductions (all threads get the result)
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
+  return x;
+}
+template <class X>
+__device__ __forceinline__ X wave_sum(X x) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+  return x;
+}
+template <int NT>
+__device__ __forceinline__ float block_max(float x, float* sh) {
+  x = wave_max(x);
+  if constexpr (NT > 64) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = sh[0];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) x = fmaxf(x, sh[w]);
+  }
+  return x;
+}
+template <int NT, class X>
+__device__ __forceinline__ X block_sum(X x, X* sh) {
+  x = wave_sum(x);
+  if constexpr (NT > 64) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = sh[0];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) x += sh[w];
+  }
+  return x;
+}
+
+struct Teach {
+  RowArr ids, t, lse;
+  int32_t top, id64, ttype;
+  double hard, denom;
+  const int* count;
+  float* losses;       // a row's loss
+};
+
+// ---------------------------------------------------------------------------
+// a row in 16-byte pieces
+// ---------------------------------------------------------------------------
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// rows start wherever V elements of the row before ended
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+
+template <class T>
+struct Piece {
+  static constexpr int N = 16 / sizeof(T);
+  // a piece outside the row: -inf, of probability 0
+  static constexpr uint32_t kNone = sizeof(T) == 4 ? 0xFF800000u : std::is_same_v<T, bf16_t> ? 0xFF80FF80u : 0xFC00FC00u;
+};
+template <class T>
+__device__ __forceinline__ u32x4 piece_none() {
+  constexpr uint32_t x = Piece<T>::kNone;
+  return u32x4{x, x, x, x};
+}
+template <class T>
+__device__ __forceinline__ u32x4 ld_piece(const T* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p));
+}
+template <class T>
+__device__ __forceinline__ void st_piece(T* p, u32x4 x) {
+  __builtin_nontemporal_store(x, reinterpret_cast<u32x4_any*>(p));
+}
+template <class T>
+__device__ __forceinline__ void unpack(u32x4 x, float (&f)[Piece<T>::N]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      f[i] = __uint_as_float(x[i]);
+    } else if constexpr (std::is_same_v<T, bf16_t>) {
+      f[2 * i] = __uint_as_float(x[i] << 16);
+      f[2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
+    } else {
+      f[2 * i] = (float)__builtin_bit_cast(f16_t, (uint16_t)(x[i] & 0xFFFFu));
+      f[2 * i + 1] = (float)__builtin_bit_cast(f16_t, (uint16_t)(x[i] >> 16));
+    }
+  }
+}
+template <class T>
+__device__ __forceinline__ u32x4 pack(const float (&f)[Piece<T>::N]) {
+  u32x4 x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      x[i] = __float_as_uint(f[i]);
+    } else if constexpr (std::is_same_v<T, bf16_t>) {
+      typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+      const b2 y = {(__bf16)f[2 * i], (__bf16)f[2 * i + 1]};
+      x[i] = __builtin_bit_cast(uint32_t, y);
+    } else {
+      typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+      const h2 y = {(_Float16)f[2 * i], (_Float16)f[2 * i + 1]};
+      x[i] = __builtin_bit_cast(uint32_t, y);
+    }
+  }
+  return x;
+}
+
+// The pieces of a sweep one after the other: scheduled into each other, or
+// with the sums moved behind the sweep, they hold several unpacked pieces at
+// once, and a row of 16 pieces a thread spills.
+__device__ __forceinline__ void piece_end() { __builtin_amdgcn_sched_barrier(0); }
+__device__ __forceinline__ void piece_end(float& sum) {
+  asm volatile("" : "+v"(sum));
+  __builtin_amdgcn_sched_barrier(0);
+}
+template <int N>
+__device__ __forceinline__ float sum_of(const float (&x)[N]) {
+  if constexpr (N == 4) return (x[0] + x[1]) + (x[2] + x[3]);
+  else return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+}
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// A row of V elements over NT threads, NV pieces of 16 bytes a thread at a
+// time: piece i is element N i .. N i + N - 1, and the V mod N elements behind
+// the last whole piece go one to each of the first threads.  With KEEP the row
+// is one such chunk and stays in registers between the sweeps; without, every
+// sweep reads it again.
+template <class T, int NT, int NV, bool KEEP>
+struct RowRegs {
+  static constexpr int N = Piece<T>::N;
+  const T* z;
+  int V, whole;
+  u32x4 raw[NV];
+  float tail;
+
+  __device__ __forceinline__ void load(int base) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int i = base + v * NT + (int)threadIdx.x;
+      raw[v] = piece_none<T>();
+      if (i < whole) raw[v] = ld_piece(z + (int64_t)i * N);
+    }
+  }
+  __device__ __forceinline__ void open(const T* p, int vocab) {
+    z = p;
+    V = vocab;
+    whole = vocab / N;
+    tail = -INFINITY;
+    if ((int)threadIdx.x < V - whole * N) tail = load_z(z + (int64_t)whole * N + threadIdx.x);
+    if constexpr (KEEP) load(0);
+  }
+  // Makes the next use of the pieces unpack them anew: an unpacked row takes
+  // twice the registers (and spilled them).
+  __device__ __forceinline__ void repack() {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) asm volatile("" : "+v"(raw[v]));
+  }
+  // f(first piece of the thread) with the chunk in raw
+  template <class F>
+  __device__ __forceinline__ void chunks(F f) {
+    if constexpr (KEEP) {
+      f((int)threadIdx.x);
+      repack();
+    } else {
+      for (int base = 0; base < whole; base += NT * NV) {
+        load(base);
+        f(base + (int)threadIdx.x);
+      }
+    }
+  }
+};
+
+// writes zeros over a row
+template <class T, int NT>
+__device__ __forceinline__ void row_zero(T* dz, int V) {
+  constexpr int N = Piece<T>::N;
+  const int whole = V / N;
+  for (int i = threadIdx.x; i < whole; i += NT) st_piece(dz + (int64_t)i * N, u32x4{0u, 0u, 0u, 0u});
+  if ((int)threadIdx.x < V - whole * N) store_z(dz + (int64_t)whole * N + threadIdx.x, 0.f);
+}
+
+// ---------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------
+struct Refusal {
+  glr_status s;
+  std::string why;
+};
+
+[[noreturn]] inline void refuse(glr_status s, const char* f, ...) {
+  char buf[256];
+  va_list ap;
+  va_start(ap, f);
+  vsnprintf(buf, sizeof buf, f, ap);
+  va_end(ap);
+  throw Refusal{s, buf};
+}
+
+template <class... P, class... A>
+void launch(const char* what, void (*k)(P...), unsigned grid, unsigned block, size_t lds, void* stream, A&&... a) {
+  if (!grid) return;
+  std::tuple<P...> t(std::forward<A>(a)...);
+  std::apply(
+      [&](P&... x) {
+        void* args[] = {(void*)&x...};
+        const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(k), dim3(grid), dim3(block), args, lds,
+                                             static_cast<hipStream_t>(stream));
+        if (e != hipSuccess) {
+          (void)hipGetLastError();
+          refuse(GLR_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
+        }
+      },
+      t);
+}
+
+// every row of a call: terms, and the gradient where there is one
+void loss_rows(int dtype, const Rows& r, const Terms& a, void* stream);
+void distill_rows(int dtype, const Rows& r, const Teach& q, void* stream);
+
+}  // namespace glr

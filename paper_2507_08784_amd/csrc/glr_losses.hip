@@ -8,436 +8,12 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <string>
-#include <tuple>
-#include <utility>
 
-#include "../../include/greedylore_losses.h"
-#include "glr_internal.hpp"
+#include "glr_loss.hpp"
 
 namespace glr {
 namespace {
-
-typedef uint16_t bf16_t;
-typedef _Float16 f16_t;
-
-constexpr int kLT = 256;                        // threads of a workgroup
-constexpr int kMaxTop = 1024;
-constexpr int64_t kMaxLossVocab = (int64_t)1 << 28;
-constexpr int64_t kMaxDistillVocab = (int64_t)1 << 19;   // the list's bitmap stays within 64 KB of LDS
-constexpr double kRestFloor = 1.0 / (1 << 20);
-constexpr double kMinTemp = 1.0 / (1 << 20);
-
-__device__ __forceinline__ float load_z(const float* p) { return *p; }
-__device__ __forceinline__ float load_z(const bf16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
-__device__ __forceinline__ float load_z(const f16_t* p) { return (float)*p; }
-__device__ __forceinline__ void store_z(float* p, float x) { *p = x; }
-__device__ __forceinline__ void store_z(bf16_t* p, float x) { *p = __builtin_bit_cast(uint16_t, (__bf16)x); }
-__device__ __forceinline__ void store_z(f16_t* p, float x) { *p = (f16_t)x; }
-
-// ---------------------------------------------------------------------------
-// arguments
-// ---------------------------------------------------------------------------
-struct RowArr {
-  const void* p;
-  int64_t sb, ss;
-};
-
-struct Rows {
-  RowArr z, dz, y;
-  int64_t ignore;
-  uint32_t rows, steps;
-  int32_t V;
-  int32_t y64;
-  float c;          // log2(e) / T: exp((z - m) / T) = 2^((z - m) c)
-  double inv_t;     // 1 / T
-  double gscale;    // grad_scale / T
-};
-
-struct Seqs {
-  const void* cu;   // NULL: the batch entries
-  int32_t n;
-  int32_t cu64;
-};
-
-__device__ __forceinline__ int64_t ld_int(const void* p, int64_t i, int w64) {
-  return w64 ? static_cast<const int64_t*>(p)[i] : (int64_t) static_cast<const int32_t*>(p)[i];
-}
-// offset i of the sequences, clamped to the rows there are
-__device__ __forceinline__ uint32_t seq_off(const Seqs& q, int64_t i, uint32_t rows) {
-  const int64_t x = ld_int(q.cu, i, q.cu64);
-  return (uint32_t)(x < 0 ? 0 : x > (int64_t)rows ? (int64_t)rows : x);
-}
-// the sequence a row belongs to, -1 if none: the last one that starts at or
-// before it (empty ones before it start there too), if it reaches that far
-__device__ __forceinline__ int seq_of(const Seqs& q, uint32_t t, uint32_t rows) {
-  int lo = 0, hi = q.n;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (seq_off(q, mid, rows) <= t) lo = mid + 1;
-    else hi = mid;
-  }
-  return lo > 0 && t < seq_off(q, lo, rows) ? lo - 1 : -1;
-}
-
-struct RowPos {
-  uint32_t t, b, s;
-  __device__ __forceinline__ int64_t of(const RowArr& a) const { return (int64_t)b * a.sb + (int64_t)s * a.ss; }
-};
-__device__ __forceinline__ RowPos row_pos(const Rows& r, uint32_t t) {
-  RowPos p;
-  p.t = t;
-  p.b = t / r.steps;
-  p.s = t - p.b * r.steps;
-  return p;
-}
-__device__ __forceinline__ float ld_f(const RowArr& a, const RowPos& p) {
-  return static_cast<const float*>(a.p)[p.of(a)];
-}
-// the row's target: whether it is trained on, and the target (-1: outside the vocabulary)
-__device__ __forceinline__ bool row_target(const Rows& r, const RowPos& p, int& y) {
-  y = 0;
-  if (!r.y.p) return true;
-  const int64_t t = ld_int(r.y.p, p.of(r.y), r.y64);
-  y = t >= 0 && t < r.V ? (int)t : -1;
-  return t != r.ignore;
-}
-
-enum { OP_LOGP, OP_COEF, OP_POLICY };
-
-struct Terms {
-  // LOGP: logps, stats, weights; COEF: stats and coef (per row) or seq_coef (per sequence)
-  float* logps;
-  float* stats;
-  RowArr coef;
-  const float* seq_coef;
-  Seqs seqs;
-  // POLICY
-  RowArr old, adv, ref;
-  double low, high, kl;      // 1 - clip_low, 1 + clip_high, kl_coef
-  double denom;              // rows that share the mean; 0: *count
-  int by_seq;                // weight 1 / (seqs * count[sequence])
-  const int* count;
-  float* part;               // 3 x rows: w term, w kl, w clipped
-};
-
-// ---------------------------------------------------------------------------
-// workgroup reductions (all threads get the result)
-// ---------------------------------------------------------------------------
-__device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
-  return x;
-}
-template <class X>
-__device__ __forceinline__ X wave_sum(X x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
-  return x;
-}
-template <int NT>
-__device__ __forceinline__ float block_max(float x, float* sh) {
-  x = wave_max(x);
-  if constexpr (NT > 64) {
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = sh[0];
-#pragma unroll
-    for (int w = 1; w < NT / 64; ++w) x = fmaxf(x, sh[w]);
-  }
-  return x;
-}
-template <int NT, class X>
-__device__ __forceinline__ X block_sum(X x, X* sh) {
-  x = wave_sum(x);
-  if constexpr (NT > 64) {
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = sh[0];
-#pragma unroll
-    for (int w = 1; w < NT / 64; ++w) x += sh[w];
-  }
-  return x;
-}
-
-// ---------------------------------------------------------------------------
-// what a row's (z_y, m, s) give
-// ---------------------------------------------------------------------------
-__device__ __forceinline__ double row_logp(const Rows& r, float zy, float m, float s) {
-  return ((double)zy - (double)m) * r.inv_t - log((double)s);
-}
-
-// stores the row's terms and returns g = d loss / d lp times grad_scale / T
-template <int OP>
-__device__ __forceinline__ double row_terms(const Rows& r, const Terms& a, const RowPos& p, int seq, double lp,
-                                            float m, float s) {
-  if constexpr (OP == OP_LOGP) {
-    a.logps[p.t] = (float)lp;
-    if (a.stats) {
-      a.stats[2 * (int64_t)p.t] = m;
-      a.stats[2 * (int64_t)p.t + 1] = s;
-    }
-    return a.coef.p ? (double)ld_f(a.coef, p) * r.gscale : 0.0;
-  } else if constexpr (OP == OP_COEF) {
-    return (double)(a.seq_coef ? a.seq_coef[seq] : ld_f(a.coef, p)) * r.gscale;
-  } else {
-    double w;
-    if (a.by_seq) {
-      const int n = a.count[seq];
-      w = 1.0 / ((double)a.seqs.n * (n > 0 ? n : 1));
-    } else {
-      w = 1.0 / (a.denom > 0.0 ? a.denom : (double)(*a.count > 0 ? *a.count : 1));
-    }
-    const double A = ld_f(a.adv, p);
-    const double ratio = exp(lp - (double)ld_f(a.old, p));
-    const double in = ratio < a.low ? a.low : ratio > a.high ? a.high : ratio;   // NaN stays
-    const double u = ratio * A, v = in * A;
-    const bool cut = u > v;
-    double term = cut ? -v : -u, slope = cut ? 0.0 : -u, k = 0.0;
-    if (a.ref.p) {
-      const double d = (double)ld_f(a.ref, p) - lp, x = expm1(d);
-      k = x - d;
-      term += a.kl * k;
-      slope -= a.kl * x;
-    }
-    a.logps[p.t] = (float)lp;
-    a.part[p.t] = (float)(w * term);
-    a.part[(int64_t)r.rows + p.t] = (float)(w * k);
-    a.part[2 * (int64_t)r.rows + p.t] = cut ? (float)w : 0.f;
-    return w * slope * r.gscale;
-  }
-}
-// what a masked row leaves
-template <int OP>
-__device__ __forceinline__ void row_masked(const Rows& r, const Terms& a, const RowPos& p) {
-  if constexpr (OP == OP_LOGP) {
-    a.logps[p.t] = 0.f;
-    if (a.stats) {
-      a.stats[2 * (int64_t)p.t] = 0.f;
-      a.stats[2 * (int64_t)p.t + 1] = 1.f;
-    }
-  } else if constexpr (OP == OP_POLICY) {
-    a.logps[p.t] = 0.f;
-    for (int k = 0; k < 3; ++k) a.part[k * (int64_t)r.rows + p.t] = 0.f;
-  }
-}
-
-// ---------------------------------------------------------------------------
-// one workgroup a row
-// ---------------------------------------------------------------------------
-template <class T, int OP>
-__global__ void __launch_bounds__(kLT) k_loss_row(Rows r, Terms a) {
-  __shared__ float sh[kLT / 64];
-  __shared__ float coef[2];
-  const RowPos p = row_pos(r, blockIdx.x);
-  int y;
-  bool live = row_target(r, p, y);
-  int seq = (int)p.b;
-  if (live && a.seqs.cu) {
-    seq = seq_of(a.seqs, p.t, r.rows);
-    live = seq >= 0;
-  }
-  T* dz = r.dz.p ? static_cast<T*>(const_cast<void*>(r.dz.p)) + p.of(r.dz) : nullptr;
-  if (!live) {
-    if (threadIdx.x == 0) row_masked<OP>(r, a, p);
-    if (dz)
-      for (int j = threadIdx.x; j < r.V; j += kLT) store_z(dz + j, 0.f);
-    return;
-  }
-  const T* z = static_cast<const T*>(r.z.p) + p.of(r.z);
-  const float zy = y >= 0 ? load_z(z + y) : __builtin_nanf("");
-  float m, s;
-  if constexpr (OP == OP_COEF) {
-    m = a.stats[2 * (int64_t)p.t];
-    s = a.stats[2 * (int64_t)p.t + 1];
-  } else {
-    m = -INFINITY;
-    for (int j = threadIdx.x; j < r.V; j += kLT) m = fmaxf(m, load_z(z + j));
-    m = block_max<kLT>(m, sh);
-    s = 0.f;
-    for (int j = threadIdx.x; j < r.V; j += kLT) s += __builtin_amdgcn_exp2f((load_z(z + j) - m) * r.c);
-    s = block_sum<kLT>(s, sh);
-  }
-  if (threadIdx.x == 0) {
-    const double lp = row_logp(r, zy, m, s);
-    const double g = row_terms<OP>(r, a, p, seq, lp, m, s);
-    coef[0] = y >= 0 ? (float)(g / (double)s) : __builtin_nanf("");
-    coef[1] = (float)g;
-  }
-  if (!dz) return;
-  __syncthreads();
-  const float f = coef[0], g = coef[1];
-  for (int j = threadIdx.x; j < r.V; j += kLT) {
-    const float e = __builtin_amdgcn_exp2f((load_z(z + j) - m) * r.c);
-    store_z(dz + j, fmaf(-f, e, j == y ? g : 0.f));
-  }
-}
-
-// ---------------------------------------------------------------------------
-// distillation
-// ---------------------------------------------------------------------------
-struct Teach {
-  RowArr ids, t, lse;
-  int32_t top, id64, ttype;
-  double hard, denom;
-  const int* count;
-  float* losses;       // a row's loss
-};
-
-__device__ __forceinline__ float ld_teacher(const Teach& q, int64_t at, int k) {
-  if (q.ttype == GLR_F32) return static_cast<const float*>(q.t.p)[at + k];
-  if (q.ttype == GLR_BF16) return load_z(static_cast<const bf16_t*>(q.t.p) + at + k);
-  return load_z(static_cast<const f16_t*>(q.t.p) + at + k);
-}
-
-// One workgroup a row.  The list's tokens are marked in a bitmap over the
-// vocabulary: the mass outside the list is summed as such (the total less the
-// list's would cancel where the list holds nearly all of it), and a repeated
-// token is seen.
-template <class T>
-__global__ void __launch_bounds__(kLT) k_distill_row(Rows r, Teach q) {
-  extern __shared__ uint32_t bits[];
-  __shared__ float shf[kLT / 64];
-  __shared__ double shd[kLT / 64];
-  __shared__ int id_s[kMaxTop];
-  __shared__ float zk_s[kMaxTop], p_s[kMaxTop];
-  __shared__ int bad_s, again_s;
-  const RowPos p = row_pos(r, blockIdx.x);
-  int y;
-  const bool live = row_target(r, p, y);
-  T* dz = r.dz.p ? static_cast<T*>(const_cast<void*>(r.dz.p)) + p.of(r.dz) : nullptr;
-  if (!live) {
-    if (threadIdx.x == 0) q.losses[p.t] = 0.f;
-    if (dz)
-      for (int j = threadIdx.x; j < r.V; j += kLT) store_z(dz + j, 0.f);
-    return;
-  }
-  const T* z = static_cast<const T*>(r.z.p) + p.of(r.z);
-  for (int j = threadIdx.x; j < (r.V + 31) / 32; j += kLT) bits[j] = 0u;
-  if (threadIdx.x == 0) bad_s = again_s = 0;
-  __syncthreads();
-  const int64_t ido = p.of(q.ids), to = p.of(q.t);
-  int have = 0, distinct = 0;
-  float high = -INFINITY;
-  for (int k = threadIdx.x; k < q.top; k += kLT) {
-    const int64_t id = ld_int(q.ids.p, ido + k, q.id64);
-    const float t = ld_teacher(q, to, k);
-    int at = -1;
-    if (id >= r.V) {
-      bad_s = 1;
-    } else if (id >= 0 && t != -INFINITY) {
-      at = (int)id;
-      const uint32_t bit = 1u << (at & 31);
-      if (atomicOr(&bits[at >> 5], bit) & bit) again_s = 1;
-      else ++distinct;
-      ++have;
-      high = fmaxf(high, t);
-    }
-    id_s[k] = at;
-    p_s[k] = t;
-    zk_s[k] = at >= 0 ? load_z(z + at) : 0.f;
-  }
-  have = block_sum<kLT, int>(have, reinterpret_cast<int*>(shf));
-  distinct = block_sum<kLT, int>(distinct, reinterpret_cast<int*>(shf));
-  high = block_max<kLT>(high, shf);
-  const bool rest = q.lse.p != nullptr && have > 0 && distinct < r.V;
-  const bool two = q.hard > 0.0 && r.inv_t != 1.0;
-  const float c1 = 1.44269504088896340736f;
-
-  float m = -INFINITY;
-  for (int j = threadIdx.x; j < r.V; j += kLT) m = fmaxf(m, load_z(z + j));
-  m = block_max<kLT>(m, shf);
-  float s = 0.f, so = 0.f, s1 = 0.f;
-  for (int j = threadIdx.x; j < r.V; j += kLT) {
-    const float d = load_z(z + j) - m, e = __builtin_amdgcn_exp2f(d * r.c);
-    s += e;
-    if (rest && !(bits[j >> 5] >> (j & 31) & 1u)) so += e;
-    if (two) s1 += __builtin_amdgcn_exp2f(d * c1);
-  }
-  s = block_sum<kLT>(s, shf);
-  if (rest) so = block_sum<kLT>(so, shf);
-  s1 = two ? block_sum<kLT>(s1, shf) : s;
-
-  // the teacher's masses and their divergence
-  const double logs = log((double)s);
-  double norm;
-  if (q.lse.p) {
-    norm = ld_f(q.lse, p);
-  } else {
-    double sum = 0.0;
-    for (int k = threadIdx.x; k < q.top; k += kLT)
-      if (id_s[k] >= 0) sum += exp(((double)p_s[k] - (double)high) * r.inv_t);
-    norm = (double)high * r.inv_t + log(block_sum<kLT, double>(sum, shd));
-  }
-  double kl = 0.0, mass = 0.0;
-  for (int k = threadIdx.x; k < q.top; k += kLT) {
-    double pk = 0.0;
-    if (id_s[k] >= 0) {
-      const double lpk = (double)p_s[k] * r.inv_t - norm;
-      pk = exp(lpk);
-      if (pk > 0.0) kl += pk * (lpk - (((double)zk_s[k] - (double)m) * r.inv_t - logs));
-      else kl += pk;        // (NaN stays)
-    }
-    p_s[k] = (float)pk;
-    mass += pk;
-  }
-  kl = block_sum<kLT, double>(kl, shd);
-  mass = block_sum<kLT, double>(mass, shd);
-  double left = 0.0;
-  if (rest) {
-    left = 1.0 - mass;
-    if (left < kRestFloor) left = 0.0;
-    if (left != 0.0) kl += left * (log(left) - (log((double)so) - logs));
-  }
-  double row = (1.0 - q.hard) * kl / (r.inv_t * r.inv_t);
-  const float nan = __builtin_nanf("");
-  if (q.hard > 0.0) {
-    const float zy = y >= 0 ? load_z(z + y) : nan;
-    row -= q.hard * ((double)zy - (double)m - log((double)s1));
-  }
-  const bool bad = bad_s != 0 || y < 0;
-  if (threadIdx.x == 0) q.losses[p.t] = bad ? nan : (float)row;
-  if (!dz) return;
-  const double n = q.denom > 0.0 ? q.denom : (double)(q.count ? (*q.count > 0 ? *q.count : 1) : r.rows);
-  const double scale = r.gscale / r.inv_t / n;     // grad_scale / n
-  const double soft = (1.0 - q.hard) / r.inv_t * scale;
-  const float f_out = bad ? nan : (float)(soft * ((mass + left) / (double)s - (left != 0.0 ? left / (double)so : 0.0)));
-  const float f_in = (float)(soft * (mass + left) / (double)s);
-  const float f1 = (float)(q.hard * scale / (double)s1), h = (float)(q.hard * scale), sf = (float)soft;
-  for (int j = threadIdx.x; j < r.V; j += kLT) {
-    const float d = load_z(z + j) - m;
-    float x = f_out * __builtin_amdgcn_exp2f(d * r.c);
-    if (q.hard > 0.0) {
-      x = fmaf(f1, __builtin_amdgcn_exp2f(d * c1), x);
-      if (j == y) x -= h;
-    }
-    if (bits[j >> 5] >> (j & 31) & 1u) continue;
-    store_z(dz + j, x);
-  }
-  for (int k = threadIdx.x; k < q.top; k += kLT) {
-    const int j = id_s[k];
-    if (j < 0) continue;
-    float mine = p_s[k];
-    if (again_s) {             // a repeated token: its first entry has the sum of its masses
-      bool first = true;
-      for (int i = 0; i < k; ++i) first = first && id_s[i] != j;
-      if (!first) continue;
-      for (int i = k + 1; i < q.top; ++i)
-        if (id_s[i] == j) mine += p_s[i];
-    }
-    const float d = zk_s[k] - m;
-    float x = fmaf(f_in, __builtin_amdgcn_exp2f(d * r.c), -sf * mine);
-    if (q.hard > 0.0) {
-      x = fmaf(f1, __builtin_amdgcn_exp2f(d * c1), x);
-      if (j == y) x -= h;
-    }
-    store_z(dz + j, bad ? nan : x);
-  }
-}
 
 // ---------------------------------------------------------------------------
 // counts, pairs and totals
@@ -550,20 +126,6 @@ __global__ void __launch_bounds__(kLT) k_loss_rescale(T* x, int64_t n, const flo
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
-struct Refusal {
-  glr_status s;
-  std::string why;
-};
-
-[[noreturn]] void refuse(glr_status s, const char* f, ...) {
-  char buf[256];
-  va_list ap;
-  va_start(ap, f);
-  vsnprintf(buf, sizeof buf, f, ap);
-  va_end(ap);
-  throw Refusal{s, buf};
-}
-
 // a C entry: nothing is thrown across it
 template <class F>
 glr_status entry(F&& body) {
@@ -579,23 +141,6 @@ glr_status entry(F&& body) {
   } catch (...) {
     return GLR_ERR_DEVICE;
   }
-}
-
-template <class... P, class... A>
-void launch(const char* what, void (*k)(P...), unsigned grid, unsigned block, size_t lds, void* stream, A&&... a) {
-  if (!grid) return;
-  std::tuple<P...> t(std::forward<A>(a)...);
-  std::apply(
-      [&](P&... x) {
-        void* args[] = {(void*)&x...};
-        const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(k), dim3(grid), dim3(block), args, lds,
-                                             static_cast<hipStream_t>(stream));
-        if (e != hipSuccess) {
-          (void)hipGetLastError();
-          refuse(GLR_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
-        }
-      },
-      t);
 }
 
 RowArr arr(const glr_row_array& a) { return RowArr{a.data, a.stride_b, a.stride_s}; }
@@ -693,12 +238,6 @@ char* check_ws(const Scratch& s, void* ws, size_t bytes) {
   return static_cast<char*>(ws);
 }
 
-template <int OP>
-void run_rows(int dtype, const Rows& r, const Terms& a, void* stream) {
-  auto* k = dtype == GLR_F32 ? k_loss_row<float, OP> : dtype == GLR_BF16 ? k_loss_row<bf16_t, OP> : k_loss_row<f16_t, OP>;
-  launch("loss rows", k, r.rows, kLT, 0, stream, r, a);
-}
-
 }  // namespace
 }  // namespace glr
 
@@ -729,10 +268,11 @@ glr_status glr_token_logprobs(const glr_loss_rows* rows, const glr_row_array* we
       check_array(*weights, 4, "weights");
     }
     Terms a = {};
+    a.op = OP_LOGP;
     a.logps = logps;
     a.stats = stats;
     if (r.dz.p) a.coef = arr(*weights);
-    run_rows<OP_LOGP>(rows->dtype, r, a, stream);
+    loss_rows(rows->dtype, r, a, stream);
   });
 }
 
@@ -746,9 +286,10 @@ glr_status glr_token_logprobs_backward(const glr_loss_rows* rows, const float* s
     if (!grad_logps) refuse(GLR_ERR_INVALID_ARG, "grad_logps is NULL");
     check_array(*grad_logps, 4, "grad_logps");
     Terms a = {};
+    a.op = OP_COEF;
     a.stats = const_cast<float*>(stats);
     a.coef = arr(*grad_logps);
-    run_rows<OP_COEF>(rows->dtype, r, a, stream);
+    loss_rows(rows->dtype, r, a, stream);
   });
 }
 
@@ -772,12 +313,13 @@ glr_status glr_preference_loss(const glr_loss_rows* rows, const glr_pref_args* x
     const Scratch s = scratch_of(GLR_LOSS_PREFERENCE, r.rows, q.n, r.dz.p != nullptr);
     char* ws = check_ws(s, d_ws, ws_bytes);
     Terms a = {};
+    a.op = OP_LOGP;
     a.seqs = q;
     a.logps = reinterpret_cast<float*>(ws + s.lp);
     a.stats = r.dz.p ? reinterpret_cast<float*>(ws + s.stats) : nullptr;
     Rows f = r;
     f.dz.p = nullptr;
-    run_rows<OP_LOGP>(rows->dtype, f, a, stream);
+    loss_rows(rows->dtype, f, a, stream);
     Pairs b = {};
     b.seqs = q;
     b.kind = x->kind;
@@ -794,8 +336,9 @@ glr_status glr_preference_loss(const glr_loss_rows* rows, const glr_pref_args* x
     launch("loss total", k_loss_total, 1, 1024, 0, stream, b.part, (int64_t)(q.n / 2), (double)(q.n / 2), nullptr,
            x->loss, nullptr, nullptr);
     if (r.dz.p) {
+      a.op = OP_COEF;
       a.seq_coef = b.coef;
-      run_rows<OP_COEF>(rows->dtype, r, a, stream);
+      loss_rows(rows->dtype, r, a, stream);
     }
   });
 }
@@ -831,6 +374,7 @@ glr_status glr_policy_loss(const glr_loss_rows* rows, const glr_policy_args* x, 
     const Scratch s = scratch_of(GLR_LOSS_POLICY, r.rows, by_seq ? q.n : 0, r.dz.p != nullptr);
     char* ws = check_ws(s, d_ws, ws_bytes);
     Terms a = {};
+    a.op = OP_POLICY;
     a.seqs = q;
     a.logps = x->logps;
     a.old = arr(x->old_logps);
@@ -845,7 +389,7 @@ glr_status glr_policy_loss(const glr_loss_rows* rows, const glr_policy_args* x, 
     a.count = count;
     a.part = reinterpret_cast<float*>(ws + s.part);
     if (by_seq || a.denom == 0.0) launch("loss count", k_loss_count, by_seq ? q.n : 1, 1024, 0, stream, r, q, (int)by_seq, count);
-    run_rows<OP_POLICY>(rows->dtype, r, a, stream);
+    loss_rows(rows->dtype, r, a, stream);
     launch("loss total", k_loss_total, 3, 1024, 0, stream, a.part, (int64_t)r.rows, 1.0, nullptr, x->loss, x->kl,
            x->clipped);
   });
@@ -889,8 +433,7 @@ glr_status glr_distill_loss(const glr_loss_rows* rows, const glr_distill_args* x
     q.count = counted ? count : nullptr;
     q.losses = x->losses;
     if (counted) launch("loss count", k_loss_count, 1, 1024, 0, stream, r, Seqs{}, 0, count);
-    auto* k = rows->dtype == GLR_F32 ? k_distill_row<float> : rows->dtype == GLR_BF16 ? k_distill_row<bf16_t> : k_distill_row<f16_t>;
-    launch("distillation rows", k, r.rows, kLT, ((size_t)r.V + 31) / 32 * 4, stream, r, q);
+    distill_rows(rows->dtype, r, q, stream);
     const double denom = counted ? 0.0 : q.denom > 0.0 ? q.denom : r.rows ? (double)r.rows : 1.0;
     launch("loss total", k_loss_total, 1, 1024, 0, stream, x->losses, (int64_t)r.rows, denom, count, x->loss, nullptr,
            nullptr);
