@@ -232,7 +232,7 @@ class _Call:
 
 def _records(logits, grad):
     """Whether a call is part of the graph (and not an explicit one)."""
-    return not grad and logits.requires_grad and torch.is_grad_enabled()
+    return not grad and torch.is_tensor(logits) and logits.requires_grad and torch.is_grad_enabled()
 
 
 # ----------------------------------------------------------------------------

@@ -1,0 +1,187 @@
+"""Host-side checks of the losses (no GPU needed): the library exports what
+include/greedylore_losses.h declares, the binding's structs have the C
+layout, and every bad argument is refused before anything touches a device,
+at the C entries and in Python."""
+import ctypes
+import os
+import re
+import shutil
+import subprocess
+
+import pytest
+import torch
+
+import paper_2507_08784_amd as glr
+from paper_2507_08784_amd import losses
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "greedylore_losses.h")
+PTR = 0x10000       # aligned, never followed
+
+
+def test_library_exports_every_declared_symbol():
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = set(re.findall(r"\b(glr_[a-z_0-9]+)\s*\(", text))
+    assert names == set(losses.LOSS_EXPORTED)
+    lib = glr.load()
+    for name in names:
+        assert hasattr(lib, name), name
+
+
+def test_struct_layouts_match_the_header(tmp_path):
+    pairs = [("glr_row_array", losses.RowArray), ("glr_loss_rows", losses.Rows), ("glr_loss_seqs", losses.Seqs),
+             ("glr_pref_args", losses.PrefArgs), ("glr_policy_args", losses.PolicyArgs),
+             ("glr_distill_args", losses.DistillArgs)]
+    lines = []
+    for c, py in pairs:
+        lines.append(f'printf("{c} %zu\\n", sizeof({c}));')
+        lines += [f'printf("{c}.{f[0]} %zu\\n", offsetof({c}, {f[0]}));' for f in py._fields_]
+    src = tmp_path / "layout.c"
+    src.write_text(f'#include "{HEADER}"\n#include <stdio.h>\nint main(void) {{ {" ".join(lines)} return 0; }}\n')
+    exe = tmp_path / "layout"
+    subprocess.run([shutil.which("gcc") or "cc", str(src), "-o", str(exe)], check=True)
+    out = dict(l.split() for l in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.splitlines())
+    for c, py in pairs:
+        assert int(out[c]) == ctypes.sizeof(py)
+        for f in py._fields_:
+            assert int(out[f"{c}.{f[0]}"]) == getattr(py, f[0]).offset, (c, f[0])
+
+
+def _rows(**kw):
+    a = dict(batch=2, steps=3, vocab=50, logits=(PTR, 150, 50), dlogits=(PTR, 150, 50), dtype=0, target_type=1,
+             targets=(PTR, 3, 1), ignore_index=-100, temperature=1.0, grad_scale=1.0)
+    a.update(kw)
+    return losses.Rows(*[a[f[0]] for f in losses.Rows._fields_])
+
+
+def _pref(**kw):
+    a = dict(seqs=(2, None, 0), kind=0, average=0, beta=0.1, label_smoothing=0.0, ref_logps=PTR, loss=PTR, logps=PTR,
+             rewards=PTR)
+    a.update(kw)
+    return losses.PrefArgs(*[a[f[0]] for f in losses.PrefArgs._fields_])
+
+
+def _policy(**kw):
+    a = dict(seqs=(2, None, 0), reduction=0, clip_low=0.2, clip_high=0.2, kl_coef=0.0, denominator=0.0,
+             old_logps=(PTR, 3, 1), advantages=(PTR, 3, 1), ref_logps=(None, 0, 0), loss=PTR, kl=PTR, clipped=PTR,
+             logps=PTR)
+    a.update(kw)
+    return losses.PolicyArgs(*[a[f[0]] for f in losses.PolicyArgs._fields_])
+
+
+def _distill(**kw):
+    a = dict(top=4, id_type=0, teacher_type=0, ids=(PTR, 12, 4), teacher=(PTR, 12, 4), teacher_lse=(None, 0, 0),
+             hard_weight=0.0, denominator=0.0, loss=PTR, losses=PTR)
+    a.update(kw)
+    return losses.DistillArgs(*[a[f[0]] for f in losses.DistillArgs._fields_])
+
+
+WS = (PTR, 1 << 20)
+W = losses.RowArray(PTR, 3, 1)
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(batch=-1), 2), (dict(steps=-1), 2), (dict(batch=1 << 16, steps=1 << 15), 2), (dict(vocab=0), 2),
+    (dict(vocab=(1 << 28) + 1), 2), (dict(dtype=3), 1), (dict(dtype=-1), 1), (dict(target_type=2), 1),
+    (dict(temperature=0.0), 1), (dict(temperature=NAN), 1), (dict(temperature=INF), 1), (dict(temperature=-1.0), 1),
+    (dict(grad_scale=INF), 1), (dict(logits=(None, 0, 0)), 1), (dict(logits=(PTR + 2, 150, 50)), 1),
+    (dict(dlogits=(PTR + 1, 150, 50)), 1), (dict(targets=(None, 0, 0)), 1), (dict(targets=(PTR + 4, 3, 1)), 1),
+])
+def test_bad_rows_are_refused_by_every_entry(kw, code):
+    lib, r = losses._lib(), _rows(**kw)
+    assert lib.glr_token_logprobs(r, W, PTR, None, None, 0, None) == code
+    assert lib.glr_last_error(None).decode()
+    assert lib.glr_token_logprobs_backward(r, PTR, W, None) == code
+    assert lib.glr_preference_loss(r, _pref(), *WS, None) == code
+    assert lib.glr_policy_loss(r, _policy(), *WS, None) == code
+    if "targets" not in kw or kw["targets"][0]:     # distillation does without targets
+        assert lib.glr_distill_loss(r, _distill(), *WS, None) == code
+
+
+def test_null_structs_and_outputs_are_refused():
+    lib, r, n = losses._lib(), _rows(), ctypes.c_size_t()
+    assert lib.glr_loss_workspace_bytes(None, 0, 0, n) == 1
+    assert lib.glr_loss_workspace_bytes(r, 0, 0, None) == 1
+    assert lib.glr_loss_workspace_bytes(r, 9, 0, n) == 1
+    assert lib.glr_loss_workspace_bytes(r, 1, -1, n) == 2
+    assert lib.glr_token_logprobs(None, W, PTR, None, None, 0, None) == 1
+    assert lib.glr_token_logprobs(r, W, None, None, None, 0, None) == 1
+    assert lib.glr_token_logprobs(r, W, PTR, PTR + 2, None, 0, None) == 1
+    assert lib.glr_token_logprobs(r, None, PTR, None, None, 0, None) == 1      # a gradient without weights
+    assert lib.glr_token_logprobs_backward(r, None, W, None) == 1
+    assert lib.glr_token_logprobs_backward(r, PTR, None, None) == 1
+    assert lib.glr_token_logprobs_backward(_rows(dlogits=(None, 0, 0)), PTR, W, None) == 1
+    for fn in (lib.glr_preference_loss, lib.glr_policy_loss, lib.glr_distill_loss):
+        assert fn(r, None, *WS, None) == 1
+    assert lib.glr_loss_rescale(None, 4, 0, PTR, None) == 1
+    assert lib.glr_loss_rescale(PTR, -1, 0, PTR, None) == 2
+    assert lib.glr_loss_rescale(PTR, 4, 5, PTR, None) == 1
+    assert lib.glr_loss_rescale(PTR, 4, 0, None, None) == 1
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(seqs=(0, None, 0)), 2), (dict(seqs=(4, None, 0)), 1), (dict(seqs=(3, PTR, 0)), 2), (dict(seqs=(2, PTR, 7)), 1),
+    (dict(seqs=(2, PTR + 2, 0)), 1), (dict(kind=3), 1), (dict(beta=0.0), 1), (dict(beta=NAN), 1),
+    (dict(label_smoothing=1.0), 1), (dict(label_smoothing=-0.1), 1), (dict(label_smoothing=0.1, kind=1), 1),
+    (dict(ref_logps=None), 1), (dict(loss=None), 1), (dict(logps=None), 1), (dict(rewards=None), 1)])
+def test_bad_preference_arguments_are_refused(kw, code):
+    assert losses._lib().glr_preference_loss(_rows(), _pref(**kw), *WS, None) == code
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(reduction=2), 1), (dict(reduction=1, seqs=(3, None, 0)), 1), (dict(reduction=1, seqs=(0, None, 0)), 2),
+    (dict(clip_low=-0.1), 1), (dict(clip_low=1.5), 1), (dict(clip_low=NAN), 1), (dict(clip_high=-0.1), 1),
+    (dict(kl_coef=-1.0), 1), (dict(kl_coef=INF), 1), (dict(kl_coef=0.1), 1), (dict(denominator=-1.0), 1),
+    (dict(denominator=INF), 1), (dict(denominator=5.0, reduction=1), 1), (dict(old_logps=(None, 0, 0)), 1),
+    (dict(advantages=(None, 0, 0)), 1), (dict(ref_logps=(PTR + 1, 3, 1)), 1), (dict(loss=None), 1), (dict(kl=None), 1),
+    (dict(clipped=None), 1), (dict(logps=None), 1)])
+def test_bad_policy_arguments_are_refused(kw, code):
+    assert losses._lib().glr_policy_loss(_rows(), _policy(**kw), *WS, None) == code
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(top=-1), 2), (dict(top=1025), 2), (dict(id_type=2), 1), (dict(teacher_type=3), 1), (dict(ids=(None, 0, 0)), 1),
+    (dict(teacher=(None, 0, 0)), 1), (dict(teacher=(PTR + 2, 12, 4)), 1), (dict(teacher_lse=(PTR + 2, 3, 1)), 1),
+    (dict(hard_weight=-0.1), 1), (dict(hard_weight=1.1), 1), (dict(hard_weight=NAN), 1), (dict(denominator=-1.0), 1),
+    (dict(loss=None), 1), (dict(losses=None), 1)])
+def test_bad_distillation_arguments_are_refused(kw, code):
+    assert losses._lib().glr_distill_loss(_rows(), _distill(**kw), *WS, None) == code
+
+
+def test_distillation_limits():
+    lib = losses._lib()
+    assert lib.glr_distill_loss(_rows(vocab=(1 << 19) + 1), _distill(), *WS, None) == 2
+    assert lib.glr_distill_loss(_rows(targets=(None, 0, 0)), _distill(hard_weight=0.5), *WS, None) == 1
+
+
+def test_workspaces_are_checked():
+    lib, r = losses._lib(), _rows()
+    for op, fn, args, seqs in ((1, lib.glr_preference_loss, _pref(), 2), (2, lib.glr_policy_loss, _policy(), 0),
+                               (3, lib.glr_distill_loss, _distill(), 0)):
+        n = ctypes.c_size_t()
+        assert lib.glr_loss_workspace_bytes(r, op, seqs, n) == 0
+        assert n.value > 0
+        assert fn(r, args, PTR, n.value - 1, None) == 3
+        assert fn(r, args, None, n.value, None) == 1
+        assert fn(r, args, PTR + 4, n.value, None) == 1
+
+
+def test_python_refusals_need_no_gpu():
+    z, y = torch.zeros(3, 5), torch.zeros(3, dtype=torch.int64)
+    with pytest.raises(ValueError, match="GPU only"):
+        losses.token_logprobs(z, y)
+    with pytest.raises(TypeError, match="float32, bfloat16 or float16"):
+        losses.token_logprobs(z.double(), y)
+    with pytest.raises(TypeError, match="tensor"):
+        losses.token_logprobs([[0.0]], y)
+    with pytest.raises(ValueError, match="rows, vocab"):
+        losses.token_logprobs(torch.zeros(5), y)
+    with pytest.raises(ValueError, match="kind"):
+        losses.preference_loss(z, y, torch.zeros(2), kind="other")
+    with pytest.raises(ValueError, match="reduction"):
+        losses.policy_loss(z, y, torch.zeros(3), torch.zeros(3), reduction="sum")
+    with pytest.raises(ValueError, match="denominator"):
+        losses.policy_loss(z, y, torch.zeros(3), torch.zeros(3), denominator=0)
+    with pytest.raises(ValueError, match="denominator"):
+        losses.distill_loss(z, torch.zeros(3, 1, dtype=torch.int64), torch.zeros(3, 1), denominator=-1.0)
