@@ -8,64 +8,194 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
 
+// the second sum, at temperature 1 (hard labels with a temperature)
+enum { ONE_T, TWO_T, SQUARE_T };   // none; its own exponential; T = 2: the square of the first
+
 __device__ __forceinline__ float ld_teacher(const Teach& q, int64_t at, int k) {
   if (q.ttype == GLR_F32) return static_cast<const float*>(q.t.p)[at + k];
   if (q.ttype == GLR_BF16) return load_z(static_cast<const bf16_t*>(q.t.p) + at + k);
   return load_z(static_cast<const f16_t*>(q.t.p) + at + k);
 }
-
-// whether element k of piece i is outside the teacher's list
+// bit k: element k of piece i is in the teacher's list
 template <int N>
 __device__ __forceinline__ uint32_t listed_bits(const uint32_t* bits, int i) {
   return bits[i * N >> 5] >> (i * N & 31);
 }
+// e(z - m) at temperature 1, from d = z - m and e at the list's temperature
+template <int TWO>
+__device__ __forceinline__ float second(float d, float e) {
+  return TWO == SQUARE_T ? e * e : exp2_of(d * kLog2e);
+}
 
-// A workgroup a row.  The list's tokens are marked in a bitmap over the
-// vocabulary in LDS: the mass outside the list is summed as such (the total
-// less the list's would cancel where the list holds nearly all of it), and a
-// repeated token is seen.  REST: there is such a mass; TWO: hard labels at a
-// temperature other than the list's, which need a second sum.  The list's own
-// gradient elements are written over the dense ones behind a barrier.
-template <class T, bool REST, bool TWO, int NT, int NV, bool KEEP>
-__global__ void __launch_bounds__(NT) k_distill_row(Rows r, Teach q) {
-  constexpr int N = Piece<T>::N;
+// What the gradient needs of a row: element j outside the list is
+// out e_j + one e1_j, one of the list in e_j + one e1_j - soft p_j, and the
+// target has hard less.
+struct Coefs {
+  float m, out, in, one, soft, hard;
+};
+
+// A workgroup a row: the first waves have the row, the last has the teacher's list
+// (its loads, exponentials and logarithms run while the row is on its way, and
+// its fp64 takes no registers beside a row's).  The list's tokens are marked
+// in a bitmap over the vocabulary in LDS: the mass outside the list is summed
+// as such (the total less the list's would cancel where the list holds nearly
+// all of it), and a repeated token is seen.  REST: there is such a mass.  The
+// list's own gradient elements are written over the dense ones behind a
+// barrier.
+template <class T, bool REST, int TWO, int NT, int NV, bool KEEP>
+__global__ void __launch_bounds__(NT + 64) k_distill_row(Rows r, Teach q) {
+  constexpr int N = Piece<T>::N, NW = NT / 64;
   extern __shared__ uint32_t bits[];
   const int words = (r.V + 31) / 32;
   int* id_s = reinterpret_cast<int*>(bits + words);
   float* zk_s = reinterpret_cast<float*>(id_s + q.top);
   float* p_s = zk_s + q.top;
-  __shared__ float shf[NT / 64];
-  __shared__ double shd[NT / 64];
-  __shared__ int bad_s, again_s;
+  __shared__ float m_s[NW], s_s[NW], o_s[NW], u_s[NW];
+  __shared__ Coefs co;
   const RowPos p = row_pos(r, blockIdx.x);
   int y;
   const bool live = row_target(r, p, y);
   T* dz = r.dz.p ? static_cast<T*>(const_cast<void*>(r.dz.p)) + p.of(r.dz) : nullptr;
   if (!live) {
     if (threadIdx.x == 0) q.losses[p.t] = 0.f;
-    if (dz) row_zero<T, NT>(dz, r.V);
+    if (dz) row_zero<T, NT + 64>(dz, r.V);
     return;
   }
-  RowRegs<T, NT, NV, KEEP> row;
-  row.open(static_cast<const T*>(r.z.p) + p.of(r.z), r.V);
-  const T* z = row.z;
-  for (int j = threadIdx.x; j < words; j += NT) bits[j] = 0u;
-  if (threadIdx.x == 0) bad_s = again_s = 0;
-  __syncthreads();
+  const T* z = static_cast<const T*>(r.z.p) + p.of(r.z);
+  // (a scalar: the two parts meet at the same number of barriers, wave by wave)
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  if (wave < NW) {
+    // ---- the row
+    RowRegs<T, NT, NV, KEEP> row;
+    row.open(z, r.V, threadIdx.x);
+    const int tail_at = row.whole * N + (int)threadIdx.x;
+    if (REST) __syncthreads();             // the list is marked
+    float mt = row.tail, st = 0.f, ot = 0.f, ut = 0.f;
+    if (tail_at < r.V) {
+      st = mt == -INFINITY ? 0.f : exp2_of((row.tail - mt) * r.c);
+      ut = st;
+      if (REST) ot = bits[tail_at >> 5] >> (tail_at & 31) & 1u ? 0.f : st;
+    }
+    row.chunks([&](int first) {
+      float top = mt;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        float x[N];
+        unpack<T>(row.raw[v], x);
+#pragma unroll
+        for (int k = 0; k < N; ++k) top = fmaxf(top, x[k]);
+        piece_end(top);
+      }
+      const float base = top == -INFINITY ? 0.f : top;
+      const float by = exp2_of((mt - base) * r.c);
+      st *= by;
+      if (REST) ot *= by;
+      if (TWO) ut *= second<TWO>(mt - base, by);
+      mt = top;
+      row.repack();
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        float x[N];
+        unpack<T>(row.raw[v], x);
+        const int i = first + v * NT;
+        const uint32_t in = REST && i < row.whole ? listed_bits<N>(bits, i) : 0u;
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] -= base;
+        if (TWO == TWO_T) {
+          float u[N];
+#pragma unroll
+          for (int k = 0; k < N; ++k) u[k] = exp2_of(x[k] * kLog2e);
+          ut += sum_of(u);
+          piece_end(ut);
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] = exp2_of(x[k] * r.c);
+        st += sum_of(x);
+        piece_end(st);
+        if (REST) {
+          float o[N];
+#pragma unroll
+          for (int k = 0; k < N; ++k) o[k] = in >> k & 1u ? 0.f : x[k];
+          ot += sum_of(o);
+          piece_end(ot);
+        }
+        if (TWO == SQUARE_T) {
+#pragma unroll
+          for (int k = 0; k < N; ++k) x[k] *= x[k];
+          ut += sum_of(x);
+          piece_end(ut);
+        }
+      }
+    });
+    // the wave's maximum, and its sums above it
+    const float mw = wave_max(mt);
+    const float by = mt == -INFINITY ? 0.f : exp2_of((mt - mw) * r.c);
+    const float sw = wave_sum(st * by), ow = REST ? wave_sum(ot * by) : 0.f;
+    const float uw = TWO ? wave_sum(ut * (mt == -INFINITY ? 0.f : second<TWO>(mt - mw, by))) : 0.f;
+    if ((threadIdx.x & 63) == 0) {
+      m_s[wave] = mw;
+      s_s[wave] = sw;
+      if (REST) o_s[wave] = ow;
+      if (TWO) u_s[wave] = uw;
+    }
+    __syncthreads();                       // the list's wave joins the sums
+    if (!dz) return;
+    __syncthreads();                       // and has the coefficients
+    const Coefs a = co;
+    const int iy = a.hard != 0.f ? y / N : -1, ky = y % N;
+    row.chunks([&](int first) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int i = first + v * NT;
+        float x[N];
+        unpack<T>(row.raw[v], x);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          const float d = x[k] - a.m, e = exp2_of(d * r.c);
+          x[k] = a.out * e;
+          if (TWO) x[k] = fmaf(a.one, second<TWO>(d, e), x[k]);
+        }
+        if (i == iy) {
+#pragma unroll
+          for (int k = 0; k < N; ++k) x[k] -= k == ky ? a.hard : 0.f;
+        }
+        if (i < row.whole) st_piece(dz + (int64_t)i * N, pack<T>(x));
+        piece_end();
+      }
+    });
+    if (tail_at < r.V) {
+      const float d = row.tail - a.m, e = exp2_of(d * r.c);
+      float x = a.out * e;
+      if (TWO) x = fmaf(a.one, second<TWO>(d, e), x);
+      store_z(dz + tail_at, x - (tail_at == y ? a.hard : 0.f));
+    }
+    __threadfence_block();
+    __syncthreads();                       // the list's elements come on top
+    return;
+  }
+
+  // ---- the list
+  const int lane = threadIdx.x & 63;
   const int64_t ido = p.of(q.ids), to = p.of(q.t);
-  int have = 0;                       // entries, and (above 16 bits) distinct tokens
+  const float nan = __builtin_nanf("");
+  const float zy = q.hard > 0.0 && y >= 0 ? load_z(z + y) : nan;
+  const double lse = q.lse.p ? (double)ld_f(q.lse, p) : 0.0;
+  const double n = q.denom > 0.0 ? q.denom : (double)(q.count ? (*q.count > 0 ? *q.count : 1) : r.rows);
+  for (int j = lane; j < words; j += 64) bits[j] = 0u;
+  bool bad = y < 0, again = false;
+  int have = 0, distinct = 0;
   float high = -INFINITY;
-  for (int k = threadIdx.x; k < q.top; k += NT) {
+  for (int k = lane; k < q.top; k += 64) {
     const int64_t id = ld_int(q.ids.p, ido + k, q.id64);
     const float t = ld_teacher(q, to, k);
     int at = -1;
     if (id >= r.V) {
-      bad_s = 1;
+      bad = true;
     } else if (id >= 0 && t != -INFINITY) {
       at = (int)id;
       const uint32_t bit = 1u << (at & 31);
-      if (atomicOr(&bits[at >> 5], bit) & bit) again_s = 1;
-      else have += 1 << 16;
+      if (atomicOr(&bits[at >> 5], bit) & bit) again = true;
+      else ++distinct;
       ++have;
       high = fmaxf(high, t);
     }
@@ -73,192 +203,130 @@ __global__ void __launch_bounds__(NT) k_distill_row(Rows r, Teach q) {
     p_s[k] = t;
     zk_s[k] = at >= 0 ? load_z(z + at) : 0.f;
   }
-  have = block_sum<NT, int>(have, reinterpret_cast<int*>(shf));
-  high = block_max<NT>(high, shf);    // (its barriers also end the marking)
-  const bool rest = REST && (have & 0xFFFF) > 0 && (have >> 16) < r.V;
-
-  // sums of the row: all tokens, those outside the list, all at temperature 1
-  float mt = row.tail, st = 0.f, ot = 0.f, ut = 0.f;
-  const int tail_at = row.whole * N + (int)threadIdx.x;
-  if (tail_at < r.V) {
-    st = exp2_of((row.tail - mt) * r.c);
-    if (mt == -INFINITY) st = 0.f;
-    ut = st;
-    if (REST) ot = bits[tail_at >> 5] >> (tail_at & 31) & 1u ? 0.f : st;
-  }
-  row.chunks([&](int first) {
-    float top = mt;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      float x[N];
-      unpack<T>(row.raw[v], x);
-#pragma unroll
-      for (int k = 0; k < N; ++k) top = fmaxf(top, x[k]);
-      piece_end(top);
-    }
-    const float base = top == -INFINITY ? 0.f : top;
-    const float by = exp2_of((mt - base) * r.c);
-    st *= by;
-    if (REST) ot *= by;
-    if (TWO) ut *= exp2_of((mt - base) * kLog2e);
-    mt = top;
-    row.repack();
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      float x[N];
-      unpack<T>(row.raw[v], x);
-      const int i = first + v * NT;
-      const uint32_t in = REST && i < row.whole ? listed_bits<N>(bits, i) : 0u;
-#pragma unroll
-      for (int k = 0; k < N; ++k) x[k] -= base;
-      if (TWO) {
-        float u[N];
-#pragma unroll
-        for (int k = 0; k < N; ++k) u[k] = exp2_of(x[k] * kLog2e);
-        ut += sum_of(u);
-        piece_end(ut);
-      }
-#pragma unroll
-      for (int k = 0; k < N; ++k) x[k] = exp2_of(x[k] * r.c);
-      st += sum_of(x);
-      piece_end(st);
-      if (REST) {
-#pragma unroll
-        for (int k = 0; k < N; ++k) x[k] = in >> k & 1u ? 0.f : x[k];
-        ot += sum_of(x);
-        piece_end(ot);
-      }
-    }
-  });
-  const float m = block_max<NT>(mt, shf);
-  const float by = exp2_of((mt - m) * r.c);
-  const float s = block_sum<NT>(st * by, shf);
-  const float so = REST ? block_sum<NT>(ot * by, shf) : 0.f;
-  const float s1 = TWO ? block_sum<NT>(ut * exp2_of((mt - m) * kLog2e), shf) : s;
-
-  // the teacher's masses and their divergence
-  const double logs = log((double)s);
-  double norm;
-  if (q.lse.p) {
-    norm = ld_f(q.lse, p);
-  } else {
+  if (REST) __syncthreads();
+  bad = __any(bad);
+  again = __any(again);
+  have = wave_sum(have);
+  distinct = wave_sum(distinct);
+  high = wave_max(high);
+  // masses p_k; with them sum p log p, sum p z
+  double norm = lse;
+  if (!q.lse.p) {
     double sum = 0.0;
-    for (int k = threadIdx.x; k < q.top; k += NT)
+    for (int k = lane; k < q.top; k += 64)
       if (id_s[k] >= 0) sum += exp(((double)p_s[k] - (double)high) * r.inv_t);
-    norm = (double)high * r.inv_t + log(block_sum<NT, double>(sum, shd));
+    norm = (double)high * r.inv_t + log(wave_sum(sum));
   }
-  double kl = 0.0, mass = 0.0;
-  for (int k = threadIdx.x; k < q.top; k += NT) {
+  double plogp = 0.0, pz = 0.0, mass = 0.0;
+  for (int k = lane; k < q.top; k += 64) {
     double pk = 0.0;
     if (id_s[k] >= 0) {
       const double lpk = (double)p_s[k] * r.inv_t - norm;
       pk = exp(lpk);
-      if (pk > 0.0) kl += pk * (lpk - (((double)zk_s[k] - (double)m) * r.inv_t - logs));
-      else kl += pk;        // (NaN stays)
+      if (pk > 0.0) {
+        plogp += pk * lpk;
+        pz += pk * (double)zk_s[k];
+      } else {
+        plogp += pk;        // (NaN stays)
+      }
     }
     p_s[k] = (float)pk;
     mass += pk;
   }
-  kl = block_sum<NT, double>(kl, shd);
-  mass = block_sum<NT, double>(mass, shd);
+  plogp = wave_sum(plogp);
+  pz = wave_sum(pz);
+  mass = wave_sum(mass);
   double left = 0.0;
-  if (rest) {
+  if (REST && have > 0 && distinct < r.V) {
     left = 1.0 - mass;
     if (left < kRestFloor) left = 0.0;
-    if (left != 0.0) kl += left * (log(left) - (log((double)so) - logs));
   }
-  const float nan = __builtin_nanf("");
-  const bool bad = bad_s != 0 || y < 0;
-  if (threadIdx.x == 0) {
+  __syncthreads();
+  // the row's maximum and sums
+  const float mw = lane < NW ? m_s[lane] : -INFINITY;
+  const float m = wave_max(mw);
+  const float by = lane < NW ? exp2_of((mw - m) * r.c) : 0.f;       // (all -inf: NaN)
+  const double s = wave_sum(lane < NW ? s_s[lane] * by : 0.f);
+  const double so = REST ? wave_sum(lane < NW ? o_s[lane] * by : 0.f) : 0.0;
+  const double s1 = TWO ? wave_sum(lane < NW ? u_s[lane] * second<TWO>(mw - m, by) : 0.f) : s;
+  if (lane == 0) {
+    if (dz) {
+      const double scale = r.gscale / r.inv_t / n, soft = (1.0 - q.hard) / r.inv_t * scale;
+      const double is = 1.0 / s, both = soft * (mass + left) * is, one = q.hard * scale / s1;
+      co.m = m;
+      // without a second sum one exponential serves both terms
+      co.out = bad ? nan : (float)(both - (left != 0.0 ? soft * left / so : 0.0) + (TWO ? 0.0 : one));
+      co.in = (float)(both + (TWO ? 0.0 : one));
+      co.one = (float)one;
+      co.soft = (float)soft;
+      co.hard = (float)(q.hard * scale);
+    }
+  }
+  if (dz) __syncthreads();
+  if (lane == 0) {
+    const double logs = log(s);
+    // KL with log q = (z - m) / T - log s, as sums over the list
+    double kl = plogp - (pz - (double)m * mass) * r.inv_t + logs * mass;
+    if (mass == 0.0) kl = plogp;
+    if (left != 0.0) kl += left * (log(left) - log(so) + logs);
     double loss = (1.0 - q.hard) * kl / (r.inv_t * r.inv_t);
-    if (q.hard > 0.0) loss -= q.hard * ((double)(y >= 0 ? load_z(z + y) : nan) - (double)m - log((double)s1));
+    if (s != s) loss = s;
+    if (q.hard > 0.0) loss -= q.hard * ((double)zy - (double)m - log(s1));
     q.losses[p.t] = bad ? nan : (float)loss;
   }
   if (!dz) return;
-  const double n = q.denom > 0.0 ? q.denom : (double)(q.count ? (*q.count > 0 ? *q.count : 1) : r.rows);
-  const double scale = r.gscale / r.inv_t / n;     // grad_scale / n
-  const double soft = (1.0 - q.hard) / r.inv_t * scale;
-  float f_out = bad ? nan : (float)(soft * ((mass + left) / (double)s - (left != 0.0 ? left / (double)so : 0.0)));
-  float f_in = (float)(soft * (mass + left) / (double)s);
-  const float f1 = (float)(q.hard * scale / (double)s1), h = (float)(q.hard * scale), sf = (float)soft;
-  if (!TWO) {                 // one exponential serves both terms
-    f_out += f1;
-    f_in += f1;
-  }
-  // (every thread has read what it needs of the row: a gradient may replace it)
-  const int iy = q.hard > 0.0 ? y / N : -1, ky = y % N;
-  row.chunks([&](int first) {
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int i = first + v * NT;
-      float x[N];
-      unpack<T>(row.raw[v], x);
-#pragma unroll
-      for (int k = 0; k < N; ++k) {
-        const float d = x[k] - m;
-        x[k] = f_out * exp2_of(d * r.c);
-        if (TWO) x[k] = fmaf(f1, exp2_of(d * kLog2e), x[k]);
-      }
-      if (i == iy) {
-#pragma unroll
-        for (int k = 0; k < N; ++k) x[k] -= k == ky ? h : 0.f;
-      }
-      if (i < row.whole) st_piece(dz + (int64_t)i * N, pack<T>(x));
-      piece_end();
-    }
-  });
-  if (tail_at < r.V) {
-    const float d = row.tail - m;
-    float x = f_out * exp2_of(d * r.c);
-    if (TWO) x = fmaf(f1, exp2_of(d * kLog2e), x);
-    store_z(dz + tail_at, x - (tail_at == y ? h : 0.f));
-  }
-  __threadfence_block();
   __syncthreads();
-  for (int k = threadIdx.x; k < q.top; k += NT) {
+  const Coefs a = co;
+  for (int k = lane; k < q.top; k += 64) {
     const int j = id_s[k];
     if (j < 0) continue;
     float mine = p_s[k];
-    if (again_s) {             // a repeated token: its first entry has the sum of its masses
+    if (again) {               // a repeated token: its first entry has the sum of its masses
       bool first = true;
       for (int i = 0; i < k; ++i) first = first && id_s[i] != j;
       if (!first) continue;
       for (int i = k + 1; i < q.top; ++i)
         if (id_s[i] == j) mine += p_s[i];
     }
-    const float d = zk_s[k] - m;
-    float x = fmaf(f_in, exp2_of(d * r.c), -sf * mine);
-    if (TWO) x = fmaf(f1, exp2_of(d * kLog2e), x);
-    if (j == y) x -= h;
+    const float d = zk_s[k] - a.m, e = exp2_of(d * r.c);
+    float x = fmaf(a.in, e, -a.soft * mine);
+    if (TWO) x = fmaf(a.one, second<TWO>(d, e), x);
+    if (j == y) x -= a.hard;
     store_z(dz + j, bad ? nan : x);
   }
 }
 
-template <class T, bool REST, bool TWO, int NT, int NV, bool KEEP>
+template <class T, bool REST, int TWO, int NT, int NV, bool KEEP>
 void go(const Rows& r, const Teach& q, void* stream) {
-  launch("distillation rows", k_distill_row<T, REST, TWO, NT, NV, KEEP>, r.rows, NT,
+  launch("distillation rows", k_distill_row<T, REST, TWO, NT, NV, KEEP>, r.rows, NT + 64,
          (((size_t)r.V + 31) / 32 + 3 * (size_t)q.top) * 4, stream, r, q);
 }
 
-template <class T, bool REST, bool TWO>
+template <class T, bool REST, int TWO>
 void rows_of(const Rows& r, const Teach& q, void* stream) {
   const int n = r.V / Piece<T>::N;          // pieces of a row
   if (n <= 128) return go<T, REST, TWO, 64, 2, true>(r, q, stream);
   if (n <= 256) return go<T, REST, TWO, 64, 4, true>(r, q, stream);
-  if (n <= 1024) return go<T, REST, TWO, 256, 4, true>(r, q, stream);
-  if (n <= 2048) return go<T, REST, TWO, 512, 4, true>(r, q, stream);
-  if (n <= 4096) return go<T, REST, TWO, 512, 8, true>(r, q, stream);
-  if (n <= 8192) return go<T, REST, TWO, 1024, 8, true>(r, q, stream);
-  if (n <= 13312) return go<T, REST, TWO, 1024, 13, true>(r, q, stream);
-  if (n <= 16384) return go<T, REST, TWO, 1024, 16, true>(r, q, stream);
-  return go<T, REST, TWO, 1024, 8, false>(r, q, stream);
+  if (n <= 768) return go<T, REST, TWO, 192, 4, true>(r, q, stream);
+  if (n <= 1792) return go<T, REST, TWO, 448, 4, true>(r, q, stream);
+  if (n <= 4032) return go<T, REST, TWO, 448, 9, true>(r, q, stream);
+  if (n <= 6720) return go<T, REST, TWO, 960, 7, true>(r, q, stream);
+  if (n <= 9600) return go<T, REST, TWO, 960, 10, true>(r, q, stream);
+  if (n <= 13440) return go<T, REST, TWO, 960, 14, true>(r, q, stream);
+  if (n <= 16320) return go<T, REST, TWO, 960, 17, true>(r, q, stream);
+  return go<T, REST, TWO, 960, 8, false>(r, q, stream);
+}
+
+template <class T, bool REST>
+void temperatures(const Rows& r, const Teach& q, void* stream) {
+  if (q.hard == 0.0 || r.inv_t == 1.0) return rows_of<T, REST, ONE_T>(r, q, stream);
+  if (r.inv_t == 0.5) return rows_of<T, REST, SQUARE_T>(r, q, stream);
+  return rows_of<T, REST, TWO_T>(r, q, stream);
 }
 
 template <class T>
 void variants(const Rows& r, const Teach& q, void* stream) {
-  const bool rest = q.lse.p != nullptr, two = q.hard > 0.0 && r.inv_t != 1.0;
-  if (rest) return two ? rows_of<T, true, true>(r, q, stream) : rows_of<T, true, false>(r, q, stream);
-  return two ? rows_of<T, false, true>(r, q, stream) : rows_of<T, false, false>(r, q, stream);
+  return q.lse.p ? temperatures<T, true>(r, q, stream) : temperatures<T, false>(r, q, stream);
 }
 
 }  // namespace

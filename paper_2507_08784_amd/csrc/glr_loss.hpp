@@ -256,24 +256,25 @@ template <class T, int NT, int NV, bool KEEP>
 struct RowRegs {
   static constexpr int N = Piece<T>::N;
   const T* z;
-  int V, whole;
+  int V, whole, tid;
   u32x4 raw[NV];
   float tail;
 
   __device__ __forceinline__ void load(int base) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int i = base + v * NT + (int)threadIdx.x;
+      const int i = base + v * NT + tid;
       raw[v] = piece_none<T>();
       if (i < whole) raw[v] = ld_piece(z + (int64_t)i * N);
     }
   }
-  __device__ __forceinline__ void open(const T* p, int vocab) {
+  __device__ __forceinline__ void open(const T* p, int vocab, int thread) {
     z = p;
     V = vocab;
+    tid = thread;
     whole = vocab / N;
     tail = -INFINITY;
-    if ((int)threadIdx.x < V - whole * N) tail = load_z(z + (int64_t)whole * N + threadIdx.x);
+    if (tid < V - whole * N) tail = load_z(z + (int64_t)whole * N + tid);
     if constexpr (KEEP) load(0);
   }
   // Makes the next use of the pieces unpack them anew: an unpacked row takes
@@ -286,12 +287,12 @@ struct RowRegs {
   template <class F>
   __device__ __forceinline__ void chunks(F f) {
     if constexpr (KEEP) {
-      f((int)threadIdx.x);
+      f(tid);
       repack();
     } else {
       for (int base = 0; base < whole; base += NT * NV) {
         load(base);
-        f(base + (int)threadIdx.x);
+        f(base + tid);
       }
     }
   }

@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(NT) k_loss_row(Rows r, Terms a) {
     return;
   }
   RowRegs<T, NT, NV, KEEP> row;
-  row.open(static_cast<const T*>(r.z.p) + p.of(r.z), r.V);
+  row.open(static_cast<const T*>(r.z.p) + p.of(r.z), r.V, threadIdx.x);
   const float zy = y >= 0 ? load_z(row.z + y) : __builtin_nanf("");
   float m, s;
   if constexpr (COEF) {
