@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(NT + 64) k_distill_row(Rows r, Teach q) {
   const float nan = __builtin_nanf("");
   const float zy = q.hard > 0.0 && y >= 0 ? load_z(z + y) : nan;
   const double lse = q.lse.p ? (double)ld_f(q.lse, p) : 0.0;
-  const double n = q.denom > 0.0 ? q.denom : (double)(q.count ? (*q.count > 0 ? *q.count : 1) : r.rows);
+  const double n = q.denom > 0.0 ? q.denom : (double)max(q.count ? *q.count : count_rows(r, Seqs{}), 1);
   for (int j = lane; j < words; j += 64) bits[j] = 0u;
   bool bad = y < 0, again = false;
   int have = 0, distinct = 0;

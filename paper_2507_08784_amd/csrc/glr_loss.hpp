@@ -22,6 +22,7 @@ typedef _Float16 f16_t;
 
 constexpr int kLT = 256;                        // threads of the small kernels
 constexpr int kMaxTop = 1024;
+constexpr uint32_t kSelfCount = 1024;           // rows that every row's own wave counts
 constexpr int64_t kMaxLossVocab = (int64_t)1 << 28;
 constexpr int64_t kMaxDistillVocab = (int64_t)1 << 19;   // the list's bitmap stays within 64 KB of LDS
 constexpr double kRestFloor = 1.0 / (1 << 20);
@@ -115,7 +116,7 @@ struct Terms {
   // POLICY
   RowArr old, adv, ref;
   double low, high, kl;      // 1 - clip_low, 1 + clip_high, kl_coef
-  double denom;              // rows that share the mean; 0: *count
+  double denom;              // rows that share the mean; 0: *count, or (NULL) as counted
   int by_seq;                // weight 1 / (seqs * count[sequence])
   const int* count;
   float* part;               // 3 x rows: w term, w kl, w clipped
@@ -166,9 +167,21 @@ struct Teach {
   RowArr ids, t, lse;
   int32_t top, id64, ttype;
   double hard, denom;
-  const int* count;
+  const int* count;    // NULL (and denom 0): as counted
   float* losses;       // a row's loss
 };
+
+// The rows trained on, by one wave: up to kSelfCount rows it takes 16 loads a
+// lane beside the row's; more are counted by a launch of their own.
+__device__ __forceinline__ int count_rows(const Rows& r, const Seqs& q) {
+  const uint32_t lo = q.cu ? seq_off(q, 0, r.rows) : 0, hi = q.cu ? seq_off(q, q.n, r.rows) : r.rows;
+  int n = 0;
+  for (uint32_t t = lo + (threadIdx.x & 63); t < hi; t += 64) {
+    int y;
+    n += row_target(r, row_pos(r, t), y);
+  }
+  return wave_sum(n);
+}
 
 // ---------------------------------------------------------------------------
 // a row in 16-byte pieces

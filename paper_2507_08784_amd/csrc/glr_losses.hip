@@ -104,15 +104,16 @@ __global__ void __launch_bounds__(kLT) k_loss_pairs(Rows r, Pairs q) {
   }
 }
 
-// out[k] = scale sum_i part[k][i]; by denom (0: *count, else 1) if there is one
-__global__ void __launch_bounds__(1024) k_loss_total(const float* part, int64_t n, double denom, const int* count,
+// out[k] = sum_t part[k][t] over the rows, by denom (0: the rows trained on)
+__global__ void __launch_bounds__(1024) k_loss_total(const float* part, Rows r, double denom, const int* count,
                                                     float* o0, float* o1, float* o2) {
   __shared__ double sh[16];
   float* out = blockIdx.x == 0 ? o0 : blockIdx.x == 1 ? o1 : o2;
   double x = 0.0;
-  for (int64_t i = threadIdx.x; i < n; i += 1024) x += part[blockIdx.x * n + i];
+  for (int64_t i = threadIdx.x; i < r.rows; i += 1024) x += part[blockIdx.x * (int64_t)r.rows + i];
   x = block_sum<1024, double>(x, sh);
-  if (threadIdx.x == 0) *out = (float)(x / (denom > 0.0 ? denom : (double)(*count > 0 ? *count : 1)));
+  if (denom == 0.0) denom = max(count ? *count : count_rows(r, Seqs{}), 1);
+  if (threadIdx.x == 0) *out = (float)(x / denom);
 }
 
 template <class T>
@@ -333,8 +334,10 @@ glr_status glr_preference_loss(const glr_loss_rows* rows, const glr_pref_args* x
     b.coef = reinterpret_cast<float*>(ws + s.coef);
     b.part = reinterpret_cast<float*>(ws + s.part);
     launch("loss pairs", k_loss_pairs, q.n / 2, kLT, 0, stream, r, b);
-    launch("loss total", k_loss_total, 1, 1024, 0, stream, b.part, (int64_t)(q.n / 2), (double)(q.n / 2), nullptr,
-           x->loss, nullptr, nullptr);
+    Rows pairs = r;
+    pairs.rows = (uint32_t)q.n / 2;
+    launch("loss total", k_loss_total, 1, 1024, 0, stream, b.part, pairs, (double)pairs.rows, nullptr, x->loss, nullptr,
+           nullptr);
     if (r.dz.p) {
       a.op = OP_COEF;
       a.seq_coef = b.coef;
@@ -386,12 +389,13 @@ glr_status glr_policy_loss(const glr_loss_rows* rows, const glr_policy_args* x, 
     a.denom = x->denominator;
     a.by_seq = by_seq;
     int* count = reinterpret_cast<int*>(ws + s.count);
-    a.count = count;
+    // (no count: each row's own wave counts)
+    const bool counted = by_seq || (a.denom == 0.0 && r.rows > kSelfCount);
+    a.count = counted ? count : nullptr;
     a.part = reinterpret_cast<float*>(ws + s.part);
-    if (by_seq || a.denom == 0.0) launch("loss count", k_loss_count, by_seq ? q.n : 1, 1024, 0, stream, r, q, (int)by_seq, count);
+    if (counted) launch("loss count", k_loss_count, by_seq ? q.n : 1, 1024, 0, stream, r, q, (int)by_seq, count);
     loss_rows(rows->dtype, r, a, stream);
-    launch("loss total", k_loss_total, 3, 1024, 0, stream, a.part, (int64_t)r.rows, 1.0, nullptr, x->loss, x->kl,
-           x->clipped);
+    launch("loss total", k_loss_total, 3, 1024, 0, stream, a.part, r, 1.0, nullptr, x->loss, x->kl, x->clipped);
   });
 }
 
@@ -420,6 +424,7 @@ glr_status glr_distill_loss(const glr_loss_rows* rows, const glr_distill_args* x
     const Scratch s = scratch_of(GLR_LOSS_DISTILL, r.rows, 0, r.dz.p != nullptr);
     char* ws = check_ws(s, d_ws, ws_bytes);
     int* count = reinterpret_cast<int*>(ws + s.count);
+    const bool all = x->denominator == 0.0 && !r.y.p;        // every row is trained on
     const bool counted = x->denominator == 0.0 && r.y.p;
     Teach q = {};
     q.ids = arr(x->ids);
@@ -429,14 +434,12 @@ glr_status glr_distill_loss(const glr_loss_rows* rows, const glr_distill_args* x
     q.id64 = x->id_type == GLR_I64;
     q.ttype = x->teacher_type;
     q.hard = x->hard_weight;
-    q.denom = x->denominator;
-    q.count = counted ? count : nullptr;
+    q.denom = all ? (double)r.rows : x->denominator;
+    q.count = counted && r.rows > kSelfCount ? count : nullptr;
     q.losses = x->losses;
-    if (counted) launch("loss count", k_loss_count, 1, 1024, 0, stream, r, Seqs{}, 0, count);
+    if (q.count) launch("loss count", k_loss_count, 1, 1024, 0, stream, r, Seqs{}, 0, count);
     distill_rows(rows->dtype, r, q, stream);
-    const double denom = counted ? 0.0 : q.denom > 0.0 ? q.denom : r.rows ? (double)r.rows : 1.0;
-    launch("loss total", k_loss_total, 1, 1024, 0, stream, x->losses, (int64_t)r.rows, denom, count, x->loss, nullptr,
-           nullptr);
+    launch("loss total", k_loss_total, 1, 1024, 0, stream, x->losses, r, q.denom, q.count, x->loss, nullptr, nullptr);
   });
 }
 
