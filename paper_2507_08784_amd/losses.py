@@ -35,6 +35,7 @@ Workspaces and results come from torch's allocator.  There is no CPU path.
 from __future__ import annotations
 
 import ctypes
+import struct
 from collections import namedtuple
 
 import torch
@@ -92,46 +93,87 @@ class DistillArgs(ctypes.Structure):
                 ("losses", _VP)]
 
 
+# The same structs as packed bytes: what a call passes (a nested ctypes struct
+# takes several microseconds to fill, about what a small launch takes).
+_ROWS = struct.Struct("@3qPqqPqqiiPqqqdd").pack
+_PREF = struct.Struct("@qPi4xiidd4P").pack
+_POLICY_ARGS = struct.Struct("@qPi4xi4x4dPqqPqqPqq4P").pack
+_DISTILL_ARGS = struct.Struct("@iii4xPqqPqqPqqdd2P").pack
+_ARRAY = struct.Struct("@Pqq").pack
+
 _fns = None
+_fast = {}
+_sizes = {}
 
 
 def _lib():
+    """The library with the losses' prototypes (structs by reference)."""
     global _fns
     if _fns is None:
         lib = load()
-        P = ctypes.POINTER
+        P, S = ctypes.POINTER, ctypes.c_size_t
         sig = {
-            "glr_loss_workspace_bytes": [P(Rows), _I32, _I64, P(ctypes.c_size_t)],
-            "glr_token_logprobs": [P(Rows), P(RowArray), _VP, _VP, _VP, ctypes.c_size_t, _VP],
+            "glr_loss_workspace_bytes": [P(Rows), _I32, _I64, P(S)],
+            "glr_token_logprobs": [P(Rows), P(RowArray), _VP, _VP, _VP, S, _VP],
             "glr_token_logprobs_backward": [P(Rows), _VP, P(RowArray), _VP],
-            "glr_preference_loss": [P(Rows), P(PrefArgs), _VP, ctypes.c_size_t, _VP],
-            "glr_policy_loss": [P(Rows), P(PolicyArgs), _VP, ctypes.c_size_t, _VP],
-            "glr_distill_loss": [P(Rows), P(DistillArgs), _VP, ctypes.c_size_t, _VP],
+            "glr_preference_loss": [P(Rows), P(PrefArgs), _VP, S, _VP],
+            "glr_policy_loss": [P(Rows), P(PolicyArgs), _VP, S, _VP],
+            "glr_distill_loss": [P(Rows), P(DistillArgs), _VP, S, _VP],
             "glr_loss_rescale": [_VP, _I64, _I32, _VP, _VP],
         }
         for name, args in sig.items():
             fn = getattr(lib, name)
             fn.restype, fn.argtypes = _I32, args
+            # and one that takes the packed structs
+            fast = lib[name]
+            fast.restype = _I32
+            fast.argtypes = [ctypes.c_char_p if a in (P(Rows), P(RowArray), P(PrefArgs), P(PolicyArgs), P(DistillArgs))
+                             else a for a in args]
+            _fast[name] = fast
         _fns = lib
     return _fns
+
+
+def _run(name, device, *args):
+    """Calls an entry on the device's current stream."""
+    if _fns is None:
+        _lib()
+    index = device.index
+    if index == torch._C._cuda_getDevice():
+        status = _fast[name](*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(device):
+            status = _fast[name](*args, torch._C._cuda_getCurrentRawStream(index))
+    if status:
+        _check(status)
+
+
+def _workspace(op, rows, count, seqs, grad, device):
+    """Scratch of a call and its size."""
+    key = (op, count, seqs, grad)
+    size = _sizes.get(key)
+    if size is None:
+        if _fns is None:
+            _lib()
+        n = ctypes.c_size_t()
+        _check(_fast["glr_loss_workspace_bytes"](rows, op, seqs, n))
+        if len(_sizes) > 4096:
+            _sizes.clear()
+        size = _sizes[key] = n.value
+    return torch.empty(size, dtype=torch.uint8, device=device), size
 
 
 # ----------------------------------------------------------------------------
 # arguments
 # ----------------------------------------------------------------------------
-_NONE = (None, 0, 0)
-
-
-def _strides(x, extra=0):
-    """(pointer, batch stride, step stride) of an array over the rows."""
-    st = x.stride()
-    if len(st) - extra == 2:
-        return x.data_ptr(), st[0], st[1]
-    return x.data_ptr(), 0, st[0]
+_NONE = (0, 0, 0)
+_FLOAT = (torch.float32,)
+_INT = (torch.int64, torch.int32)
+_ANY = (torch.float32, torch.bfloat16, torch.float16)
 
 
 def _same(x, name, shape, device, dtypes):
-    if not torch.is_tensor(x):
+    if not isinstance(x, torch.Tensor):
         raise TypeError(f"{name} must be a tensor, not {type(x).__name__}")
     if x.dtype not in dtypes:
         raise TypeError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, not {x.dtype}")
@@ -141,98 +183,77 @@ def _same(x, name, shape, device, dtypes):
         raise ValueError(f"{name} must live on {device}, not {x.device}")
 
 
-_FLOAT = (torch.float32,)
-_INT = (torch.int64, torch.int32)
-_ANY = (torch.float32, torch.bfloat16, torch.float16)
+def _array(x, name, shape, device, dtypes=_FLOAT):
+    """(pointer, batch stride, step stride) of an array over the rows."""
+    _same(x, name, shape, device, dtypes)
+    st = x.stride()
+    return (x.data_ptr(), st[0], st[1]) if len(st) == 2 else (x.data_ptr(), 0, st[0])
 
 
-class _Call:
-    """One call's rows: the checks every loss makes, and the C struct."""
+def _lists(x, name, shape, device, dtypes):
+    """The same of an array with a contiguous list in each row."""
+    _same(x, name, shape, device, dtypes)
+    st = x.stride()
+    if st[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"a row of {name} must be contiguous" + (" (stride 1 over the vocabulary)" if dtypes is _ANY else ""))
+    return (x.data_ptr(), st[0], st[1]) if len(st) == 3 else (x.data_ptr(), 0, st[0])
 
-    __slots__ = ("logits", "shape", "device", "rows", "dlogits", "keep", "batch", "steps")
 
-    def __init__(self, logits, targets, ignore_index, temperature, grad, grad_scale, out):
-        if not torch.is_tensor(logits):
-            raise TypeError(f"logits must be a tensor, not {type(logits).__name__}")
-        if logits.dtype not in _DTYPES:
-            raise TypeError(f"logits must be float32, bfloat16 or float16, not {logits.dtype}")
-        if logits.dim() not in (2, 3):
-            raise ValueError(f"logits must be (rows, vocab) or (batch, steps, vocab), not {tuple(logits.shape)}")
-        if not logits.is_cuda:
-            raise ValueError("the losses run on the GPU only (logits on the CPU)")
-        shape = logits.shape[:-1]
-        device = logits.device
-        if logits.shape[-1] > 1 and logits.stride(-1) != 1:
-            raise ValueError("a row of logits must be contiguous (stride 1 over the vocabulary)")
-        self.logits, self.shape, self.device = logits, shape, device
-        if targets is not None:
-            _same(targets, "targets", shape, device, _INT)
-        d = None
-        if out is not None and not grad:
-            raise ValueError("out is the gradient's: it needs grad=True (weights=... of token_logprobs)")
-        if grad:
-            if out is None:
-                d = torch.empty(logits.shape, dtype=logits.dtype, device=device)
-            else:
-                _same(out, "out", logits.shape, device, (logits.dtype,))
-                if out.shape[-1] > 1 and out.stride(-1) != 1:
-                    raise ValueError("a row of out must be contiguous (stride 1 over the vocabulary)")
-                if out.data_ptr() == logits.data_ptr() and out.stride() != logits.stride():
-                    raise ValueError("out that replaces the logits must have their strides")
-                d = out
-        self.dlogits = d
-        self.batch, self.steps = (shape[0], shape[1]) if len(shape) == 2 else (1, shape[0])
-        self.rows = Rows(self.batch, self.steps, logits.shape[-1], _strides(logits, 1),
-                         _strides(d, 1) if d is not None else _NONE, _DTYPES[logits.dtype],
-                         _ITYPES[targets.dtype] if targets is not None else 0,
-                         _strides(targets) if targets is not None else _NONE, ignore_index, temperature, grad_scale)
-
-    def array(self, x, name, dtypes=_FLOAT):
-        _same(x, name, self.shape, self.device, dtypes)
-        return _strides(x)
-
-    def lists(self, x, name, shape, dtypes):
-        """A per-row list: its last dimension contiguous."""
-        _same(x, name, shape, self.device, dtypes)
-        if x.shape[-1] > 1 and x.stride(-1) != 1:
-            raise ValueError(f"a row of {name} must be contiguous")
-        return _strides(x, 1)
-
-    def seqs(self, cu):
-        if cu is None:
-            if len(self.shape) != 2:
-                raise ValueError("packed rows (2-D logits) need cu_seqlens")
-            return self.batch, (self.batch, None, 0)
-        if cu.dim() != 1 or cu.numel() < 2:
-            raise ValueError("cu_seqlens must be one-dimensional with at least two offsets")
-        if len(self.shape) != 1:
-            raise ValueError("cu_seqlens goes with packed rows (2-D logits)")
-        _same(cu, "cu_seqlens", cu.shape, self.device, _INT)
-        if not cu.is_contiguous():
-            raise ValueError("cu_seqlens must be contiguous")
-        n = cu.numel() - 1
-        return n, (n, cu.data_ptr(), _ITYPES[cu.dtype])
-
-    def f32(self, *shape):
-        return torch.empty(shape, dtype=torch.float32, device=self.device)
-
-    def workspace(self, op, seqs):
-        n = ctypes.c_size_t()
-        _check(_lib().glr_loss_workspace_bytes(self.rows, op, seqs, n))
-        return torch.empty(n.value, dtype=torch.uint8, device=self.device), n.value
-
-    def run(self, fn, *args):
-        dev = self.device
-        if dev.index != torch.cuda.current_device():
-            with torch.cuda.device(dev):
-                _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+def _rows(logits, targets, ignore_index, temperature, grad, grad_scale, out):
+    """The checks that every loss makes of its rows: (packed struct, shape of
+    the rows, device, (batch, steps), gradient or None)."""
+    if not isinstance(logits, torch.Tensor):
+        raise TypeError(f"logits must be a tensor, not {type(logits).__name__}")
+    dtype = logits.dtype
+    if dtype not in _DTYPES:
+        raise TypeError(f"logits must be float32, bfloat16 or float16, not {dtype}")
+    full = logits.shape
+    if len(full) not in (2, 3):
+        raise ValueError(f"logits must be (rows, vocab) or (batch, steps, vocab), not {tuple(full)}")
+    if not logits.is_cuda:
+        raise ValueError("the losses run on the GPU only (logits on the CPU)")
+    shape, device = full[:-1], logits.device
+    z = _lists(logits, "logits", full, device, _ANY)
+    d, dz = None, _NONE
+    if grad:
+        if out is None:
+            d = torch.empty(full, dtype=dtype, device=device)
         else:
-            _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+            _same(out, "out", full, device, (dtype,))
+            if out.data_ptr() == z[0] and out.stride() != logits.stride():
+                raise ValueError("out that replaces the logits must have their strides")
+            d = out
+        dz = _lists(d, "out", full, device, _ANY)
+    elif out is not None:
+        raise ValueError("out is the gradient's: it needs grad=True (weights=... of token_logprobs)")
+    y, itype = _NONE, 0
+    if targets is not None:
+        y = _array(targets, "targets", shape, device, _INT)
+        itype = _ITYPES[targets.dtype]
+    b, s = shape if len(shape) == 2 else (1, shape[0])
+    return (_ROWS(b, s, full[-1], *z, *dz, _DTYPES[dtype], itype, *y, ignore_index, temperature, grad_scale), shape,
+            device, (b, s), d)
+
+
+def _seqs(cu, shape, device):
+    """(sequences, pointer of their offsets, type of them)."""
+    if cu is None:
+        if len(shape) != 2:
+            raise ValueError("packed rows (2-D logits) need cu_seqlens")
+        return shape[0], 0, 0
+    if cu.dim() != 1 or cu.numel() < 2:
+        raise ValueError("cu_seqlens must be one-dimensional with at least two offsets")
+    if len(shape) != 1:
+        raise ValueError("cu_seqlens goes with packed rows (2-D logits)")
+    _same(cu, "cu_seqlens", cu.shape, device, _INT)
+    if not cu.is_contiguous():
+        raise ValueError("cu_seqlens must be contiguous")
+    return cu.numel() - 1, cu.data_ptr(), _ITYPES[cu.dtype]
 
 
 def _records(logits, grad):
     """Whether a call is part of the graph (and not an explicit one)."""
-    return not grad and torch.is_tensor(logits) and logits.requires_grad and torch.is_grad_enabled()
+    return not grad and isinstance(logits, torch.Tensor) and logits.requires_grad and torch.is_grad_enabled()
 
 
 # ----------------------------------------------------------------------------
@@ -246,7 +267,7 @@ class _WithGradient(torch.autograd.Function):
     def forward(ctx, logits, compute):
         result = compute()
         ctx.dlogits = result.dlogits
-        rest = tuple(x for x in result[1:-1])
+        rest = tuple(result[1:-1])
         ctx.mark_non_differentiable(*rest)
         return (result.loss,) + rest
 
@@ -257,19 +278,20 @@ class _WithGradient(torch.autograd.Function):
         if d is None:
             raise RuntimeError("the loss's gradient was handed on already: call the loss again for a second backward")
         scale = grad_loss.float().contiguous()
-        dev = d.device
-        with torch.cuda.device(dev):
-            _check(_lib().glr_loss_rescale(d.data_ptr(), d.numel(), _DTYPES[d.dtype], scale.data_ptr(),
-                                           torch.cuda.current_stream(dev).cuda_stream))
+        if d.is_contiguous():
+            _run("glr_loss_rescale", d.device, d.data_ptr(), d.numel(), _DTYPES[d.dtype], scale.data_ptr())
+        else:                       # an `out` with room between its rows
+            d.mul_(scale)
         return d, None
 
 
 class _TokenLogprobs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, targets, temperature, ignore_index):
-        c = _Call(logits, targets, ignore_index, temperature, False, 1.0, None)
-        logps, stats = c.f32(*c.shape), c.f32(c.batch * c.steps, 2)
-        c.run(_lib().glr_token_logprobs, c.rows, None, logps.data_ptr(), stats.data_ptr(), None, 0)
+        rows, shape, device, (b, s), _ = _rows(logits, targets, ignore_index, temperature, False, 1.0, None)
+        logps = torch.empty(shape, dtype=torch.float32, device=device)
+        stats = torch.empty((b * s, 2), dtype=torch.float32, device=device)
+        _run("glr_token_logprobs", device, rows, None, logps.data_ptr(), stats.data_ptr(), None, 0)
         ctx.save_for_backward(logits, targets, stats)
         ctx.options = (ignore_index, temperature)
         return logps
@@ -278,11 +300,10 @@ class _TokenLogprobs(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad):
         logits, targets, stats = ctx.saved_tensors
-        ignore_index, temperature = ctx.options
-        c = _Call(logits, targets, ignore_index, temperature, True, 1.0, None)
-        w = RowArray(*c.array(grad, "the upstream gradient"))
-        c.run(_lib().glr_token_logprobs_backward, c.rows, stats.data_ptr(), w)
-        return c.dlogits, None, None, None
+        rows, shape, device, _, d = _rows(logits, targets, *ctx.options, True, 1.0, None)
+        w = _ARRAY(*_array(grad, "the upstream gradient", shape, device))
+        _run("glr_token_logprobs_backward", device, rows, stats.data_ptr(), w)
+        return d, None, None, None
 
 
 # ----------------------------------------------------------------------------
@@ -297,11 +318,11 @@ def token_logprobs(logits, targets, *, weights=None, temperature=1.0, ignore_ind
         if out is not None:
             raise ValueError("out needs weights")
         return TokenLogprobs(_TokenLogprobs.apply(logits, targets, temperature, ignore_index), None)
-    c = _Call(logits, targets, ignore_index, temperature, weights is not None, grad_scale, out)
-    w = RowArray(*c.array(weights, "weights")) if weights is not None else None
-    logps = c.f32(*c.shape)
-    c.run(_lib().glr_token_logprobs, c.rows, w, logps.data_ptr(), None, None, 0)
-    return TokenLogprobs(logps, c.dlogits)
+    rows, shape, device, _, d = _rows(logits, targets, ignore_index, temperature, weights is not None, grad_scale, out)
+    w = _ARRAY(*_array(weights, "weights", shape, device)) if weights is not None else None
+    logps = torch.empty(shape, dtype=torch.float32, device=device)
+    _run("glr_token_logprobs", device, rows, w, logps.data_ptr(), None, None, 0)
+    return TokenLogprobs(logps, d)
 
 
 def preference_loss(logits, targets, ref_logps, *, beta=0.1, kind="sigmoid", label_smoothing=0.0, average=False,
@@ -319,17 +340,19 @@ def preference_loss(logits, targets, ref_logps, *, beta=0.1, kind="sigmoid", lab
     record = _records(logits, grad)
 
     def compute():
-        c = _Call(logits, targets, ignore_index, 1.0, grad or record, grad_scale, out)
-        n, seqs = c.seqs(cu_seqlens)
-        _same(ref_logps, "ref_logps", (n,), c.device, _FLOAT)
+        rows, shape, device, (b, s), d = _rows(logits, targets, ignore_index, 1.0, grad or record, grad_scale, out)
+        n, *seqs = _seqs(cu_seqlens, shape, device)
+        _same(ref_logps, "ref_logps", (n,), device, _FLOAT)
         if not ref_logps.is_contiguous():
             raise ValueError("ref_logps must be contiguous")
-        loss, logps, rewards = c.f32(), c.f32(n), c.f32(n)
-        args = PrefArgs(seqs, KINDS[kind], bool(average), beta, label_smoothing, ref_logps.data_ptr(),
-                        loss.data_ptr(), logps.data_ptr(), rewards.data_ptr())
-        ws, size = c.workspace(_PREFERENCE, n)
-        c.run(_lib().glr_preference_loss, c.rows, args, ws.data_ptr(), size)
-        return PreferenceLoss(loss, logps, rewards, c.dlogits)
+        logps, rewards = torch.empty((2, n), dtype=torch.float32, device=device).unbind()
+        loss = torch.empty((), dtype=torch.float32, device=device)
+        at = logps.data_ptr()
+        args = _PREF(n, *seqs, KINDS[kind], bool(average), beta, label_smoothing, ref_logps.data_ptr(), loss.data_ptr(),
+                     at, at + 4 * n)
+        ws, size = _workspace(_PREFERENCE, rows, b * s, n, d is not None, device)
+        _run("glr_preference_loss", device, rows, args, ws.data_ptr(), size)
+        return PreferenceLoss(loss, logps, rewards, d)
 
     if record:
         return PreferenceLoss(*_WithGradient.apply(logits, compute), None)
@@ -354,18 +377,20 @@ def policy_loss(logits, targets, old_logps, advantages, *, ref_logps=None, clip_
     record = _records(logits, grad)
 
     def compute():
-        c = _Call(logits, targets, ignore_index, temperature, grad or record, grad_scale, out)
-        n, seqs = 0, (0, None, 0)
+        rows, shape, device, (b, s), d = _rows(logits, targets, ignore_index, temperature, grad or record, grad_scale, out)
+        seqs = (0, 0, 0)
         if cu_seqlens is not None or reduction == "sequence":
-            n, seqs = c.seqs(cu_seqlens)
-        old, adv = c.array(old_logps, "old_logps"), c.array(advantages, "advantages")
-        ref = c.array(ref_logps, "ref_logps") if ref_logps is not None else _NONE
-        loss, kl, clipped, logps = c.f32(), c.f32(), c.f32(), c.f32(*c.shape)
-        args = PolicyArgs(seqs, REDUCTIONS[reduction], clip_low, clip_high, kl_coef, denominator or 0.0, old, adv, ref,
-                          loss.data_ptr(), kl.data_ptr(), clipped.data_ptr(), logps.data_ptr())
-        ws, size = c.workspace(_POLICY, n)
-        c.run(_lib().glr_policy_loss, c.rows, args, ws.data_ptr(), size)
-        return PolicyLoss(loss, logps, kl, clipped, c.dlogits)
+            seqs = _seqs(cu_seqlens, shape, device)
+        old, adv = _array(old_logps, "old_logps", shape, device), _array(advantages, "advantages", shape, device)
+        ref = _array(ref_logps, "ref_logps", shape, device) if ref_logps is not None else _NONE
+        loss, kl, clipped = torch.empty(3, dtype=torch.float32, device=device).unbind()
+        logps = torch.empty(shape, dtype=torch.float32, device=device)
+        at = loss.data_ptr()
+        args = _POLICY_ARGS(*seqs, REDUCTIONS[reduction], clip_low, clip_high, kl_coef, denominator or 0.0, *old, *adv,
+                            *ref, at, at + 4, at + 8, logps.data_ptr())
+        ws, size = _workspace(_POLICY, rows, b * s, seqs[0], d is not None, device)
+        _run("glr_policy_loss", device, rows, args, ws.data_ptr(), size)
+        return PolicyLoss(loss, logps, kl, clipped, d)
 
     if record:
         return PolicyLoss(*_WithGradient.apply(logits, compute), None)
@@ -391,20 +416,21 @@ def distill_loss(logits, teacher_ids, teacher_logits, *, temperature=1.0, teache
     record = _records(logits, grad)
 
     def compute():
-        c = _Call(logits, targets, ignore_index, temperature, grad or record, grad_scale, out)
-        if not torch.is_tensor(teacher_ids) or teacher_ids.dim() != len(c.shape) + 1:
+        rows, shape, device, (b, s), d = _rows(logits, targets, ignore_index, temperature, grad or record, grad_scale, out)
+        if not isinstance(teacher_ids, torch.Tensor) or teacher_ids.dim() != len(shape) + 1:
             raise ValueError("teacher_ids must have the logits' dimensions")
         K = teacher_ids.shape[-1]
-        shape = c.shape + (K,)
-        ids = c.lists(teacher_ids, "teacher_ids", shape, _INT)
-        t = c.lists(teacher_logits, "teacher_logits", shape, _ANY)
-        lse = c.array(teacher_lse, "teacher_lse") if teacher_lse is not None else _NONE
-        loss, losses = c.f32(), c.f32(*c.shape)
-        args = DistillArgs(K, _ITYPES[teacher_ids.dtype], _DTYPES[teacher_logits.dtype], ids, t, lse, hard_weight,
-                           denominator or 0.0, loss.data_ptr(), losses.data_ptr())
-        ws, size = c.workspace(_DISTILL, 0)
-        c.run(_lib().glr_distill_loss, c.rows, args, ws.data_ptr(), size)
-        return DistillLoss(loss, losses, c.dlogits)
+        lists = shape + (K,)
+        ids = _lists(teacher_ids, "teacher_ids", lists, device, _INT)
+        t = _lists(teacher_logits, "teacher_logits", lists, device, _ANY)
+        lse = _array(teacher_lse, "teacher_lse", shape, device) if teacher_lse is not None else _NONE
+        loss = torch.empty((), dtype=torch.float32, device=device)
+        losses = torch.empty(shape, dtype=torch.float32, device=device)
+        args = _DISTILL_ARGS(K, _ITYPES[teacher_ids.dtype], _DTYPES[teacher_logits.dtype], *ids, *t, *lse, hard_weight,
+                             denominator or 0.0, loss.data_ptr(), losses.data_ptr())
+        ws, size = _workspace(_DISTILL, rows, b * s, 0, d is not None, device)
+        _run("glr_distill_loss", device, rows, args, ws.data_ptr(), size)
+        return DistillLoss(loss, losses, d)
 
     if record:
         return DistillLoss(*_WithGradient.apply(logits, compute), None)
