@@ -16,10 +16,18 @@ __device__ __forceinline__ float ld_teacher(const Teach& q, int64_t at, int k) {
   if (q.ttype == GLR_BF16) return load_z(static_cast<const bf16_t*>(q.t.p) + at + k);
   return load_z(static_cast<const f16_t*>(q.t.p) + at + k);
 }
+// The bitmap's first bit is that of the 16-byte piece in which the row begins,
+// so that no piece's bits lie in two words: element j has bit j + lead.
+template <class T>
+__device__ __forceinline__ int bit_lead(int head) {
+  return head ? Piece<T>::N - head : 0;
+}
+inline size_t bit_words(int V) { return ((size_t)V + 8 + 31) / 32; }
 // bit k: element k of piece i is in the teacher's list
 template <int N>
-__device__ __forceinline__ uint32_t listed_bits(const uint32_t* bits, int i) {
-  return bits[i * N >> 5] >> (i * N & 31);
+__device__ __forceinline__ uint32_t listed_bits(const uint32_t* bits, int i, int head) {
+  const int b = (i + (head != 0)) * N;
+  return bits[b >> 5] >> (b & 31);
 }
 // e(z - m) at temperature 1, from d = z - m and e at the list's temperature
 template <int TWO>
@@ -46,7 +54,7 @@ template <class T, bool REST, int TWO, int NT, int NV, bool KEEP>
 __global__ void __launch_bounds__(NT + 64) k_distill_row(Rows r, Teach q) {
   constexpr int N = Piece<T>::N, NW = NT / 64;
   extern __shared__ uint32_t bits[];
-  const int words = (r.V + 31) / 32;
+  const int words = (r.V + 8 + 31) / 32;
   int* id_s = reinterpret_cast<int*>(bits + words);
   float* zk_s = reinterpret_cast<float*>(id_s + q.top);
   float* p_s = zk_s + q.top;
@@ -58,7 +66,7 @@ __global__ void __launch_bounds__(NT + 64) k_distill_row(Rows r, Teach q) {
   T* dz = r.dz.p ? static_cast<T*>(const_cast<void*>(r.dz.p)) + p.of(r.dz) : nullptr;
   if (!live) {
     if (threadIdx.x == 0) q.losses[p.t] = 0.f;
-    if (dz) row_zero<T, NT + 64>(dz, r.V);
+    if (dz) row_zero<T, NT + 64>(dz, r.V, threadIdx.x);
     return;
   }
   const T* z = static_cast<const T*>(r.z.p) + p.of(r.z);
@@ -68,13 +76,11 @@ __global__ void __launch_bounds__(NT + 64) k_distill_row(Rows r, Teach q) {
     // ---- the row
     RowRegs<T, NT, NV, KEEP> row;
     row.open(z, r.V, threadIdx.x);
-    const int tail_at = row.whole * N + (int)threadIdx.x;
     if (REST) __syncthreads();             // the list is marked
-    float mt = row.tail, st = 0.f, ot = 0.f, ut = 0.f;
-    if (tail_at < r.V) {
-      st = mt == -INFINITY ? 0.f : exp2_of((row.tail - mt) * r.c);
-      ut = st;
-      if (REST) ot = bits[tail_at >> 5] >> (tail_at & 31) & 1u ? 0.f : st;
+    float mt = row.end, st = mt == -INFINITY ? 0.f : exp2_of((row.end - mt) * r.c), ot = 0.f, ut = st;
+    if (REST && row.at >= 0) {
+      const int b = row.at + bit_lead<T>(row.head);
+      ot = bits[b >> 5] >> (b & 31) & 1u ? 0.f : st;
     }
     row.chunks([&](int first) {
       float top = mt;
@@ -98,7 +104,7 @@ __global__ void __launch_bounds__(NT + 64) k_distill_row(Rows r, Teach q) {
         float x[N];
         unpack<T>(row.raw[v], x);
         const int i = first + v * NT;
-        const uint32_t in = REST && i < row.whole ? listed_bits<N>(bits, i) : 0u;
+        const uint32_t in = REST && i < row.whole ? listed_bits<N>(bits, i, row.head) : 0u;
 #pragma unroll
         for (int k = 0; k < N; ++k) x[k] -= base;
         if (TWO == TWO_T) {
@@ -142,7 +148,8 @@ __global__ void __launch_bounds__(NT + 64) k_distill_row(Rows r, Teach q) {
     if (!dz) return;
     __syncthreads();                       // and has the coefficients
     const Coefs a = co;
-    const int iy = a.hard != 0.f ? y / N : -1, ky = y % N;
+    const int py = a.hard != 0.f ? y - row.head : -1;      // the target's place among the pieces
+    const int iy = py >= 0 ? py / N : -1, ky = py % N;
     row.chunks([&](int first) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
@@ -159,15 +166,15 @@ __global__ void __launch_bounds__(NT + 64) k_distill_row(Rows r, Teach q) {
 #pragma unroll
           for (int k = 0; k < N; ++k) x[k] -= k == ky ? a.hard : 0.f;
         }
-        if (i < row.whole) st_piece(dz + (int64_t)i * N, pack<T>(x));
+        if (i < row.whole) st_piece(dz + row.head + (int64_t)i * N, pack<T>(x));
         piece_end();
       }
     });
-    if (tail_at < r.V) {
-      const float d = row.tail - a.m, e = exp2_of(d * r.c);
+    if (row.at >= 0) {
+      const float d = row.end - a.m, e = exp2_of(d * r.c);
       float x = a.out * e;
       if (TWO) x = fmaf(a.one, second<TWO>(d, e), x);
-      store_z(dz + tail_at, x - (tail_at == y ? a.hard : 0.f));
+      store_z(dz + row.at, x - (row.at == y ? a.hard : 0.f));
     }
     __threadfence_block();
     __syncthreads();                       // the list's elements come on top
@@ -182,6 +189,7 @@ __global__ void __launch_bounds__(NT + 64) k_distill_row(Rows r, Teach q) {
   const double lse = q.lse.p ? (double)ld_f(q.lse, p) : 0.0;
   const double n = q.denom > 0.0 ? q.denom : (double)max(q.count ? *q.count : count_rows(r, Seqs{}), 1);
   for (int j = lane; j < words; j += 64) bits[j] = 0u;
+  const int lead = bit_lead<T>(Cut<T>(z, r.V).head);
   bool bad = y < 0, again = false;
   int have = 0, distinct = 0;
   float high = -INFINITY;
@@ -193,8 +201,9 @@ __global__ void __launch_bounds__(NT + 64) k_distill_row(Rows r, Teach q) {
       bad = true;
     } else if (id >= 0 && t != -INFINITY) {
       at = (int)id;
-      const uint32_t bit = 1u << (at & 31);
-      if (atomicOr(&bits[at >> 5], bit) & bit) again = true;
+      const int b = at + lead;
+      const uint32_t bit = 1u << (b & 31);
+      if (atomicOr(&bits[b >> 5], bit) & bit) again = true;
       else ++distinct;
       ++have;
       high = fmaxf(high, t);
@@ -299,7 +308,7 @@ __global__ void __launch_bounds__(NT + 64) k_distill_row(Rows r, Teach q) {
 template <class T, bool REST, int TWO, int NT, int NV, bool KEEP>
 void go(const Rows& r, const Teach& q, void* stream) {
   launch("distillation rows", k_distill_row<T, REST, TWO, NT, NV, KEEP>, r.rows, NT + 64,
-         (((size_t)r.V + 31) / 32 + 3 * (size_t)q.top) * 4, stream, r, q);
+         (bit_words(r.V) + 3 * (size_t)q.top) * 4, stream, r, q);
 }
 
 template <class T, bool REST, int TWO>

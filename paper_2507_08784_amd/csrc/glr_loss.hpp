@@ -125,16 +125,51 @@ struct Terms {
 // ---------------------------------------------------------------------------
 // workgroup reductions (all threads get the result)
 // ---------------------------------------------------------------------------
+// Within a wave by data-parallel moves (a shuffle through LDS takes many times
+// their latency): sums of 2, 4, 8, 16 lanes, of two and four such rows, and the
+// last lane's value to all.
+template <int CTRL, int ROWS, class X>
+__device__ __forceinline__ X dpp_move(X other, X x) {
+  if constexpr (sizeof(X) == 4) {
+    return __builtin_bit_cast(X, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, other), __builtin_bit_cast(int, x), CTRL,
+                                                            ROWS, 0xF, false));
+  } else {
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    const i32x2 o = __builtin_bit_cast(i32x2, other), v = __builtin_bit_cast(i32x2, x);
+    const i32x2 y = {__builtin_amdgcn_update_dpp(o[0], v[0], CTRL, ROWS, 0xF, false),
+                     __builtin_amdgcn_update_dpp(o[1], v[1], CTRL, ROWS, 0xF, false)};
+    return __builtin_bit_cast(X, y);
+  }
+}
+template <class X>
+__device__ __forceinline__ X lane_value(X x, int lane) {
+  if constexpr (sizeof(X) == 4) {
+    return __builtin_bit_cast(X, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+  } else {
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    const i32x2 v = __builtin_bit_cast(i32x2, x);
+    const i32x2 y = {__builtin_amdgcn_readlane(v[0], lane), __builtin_amdgcn_readlane(v[1], lane)};
+    return __builtin_bit_cast(X, y);
+  }
+}
 __device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
-  return x;
+  x = fmaxf(x, dpp_move<0x111, 0xF>(x, x));   // row_shr:1
+  x = fmaxf(x, dpp_move<0x112, 0xF>(x, x));
+  x = fmaxf(x, dpp_move<0x114, 0xF>(x, x));
+  x = fmaxf(x, dpp_move<0x118, 0xF>(x, x));
+  x = fmaxf(x, dpp_move<0x142, 0xA>(x, x));   // row_bcast:15
+  x = fmaxf(x, dpp_move<0x143, 0xC>(x, x));   // row_bcast:31
+  return lane_value(x, 63);
 }
 template <class X>
 __device__ __forceinline__ X wave_sum(X x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
-  return x;
+  x += dpp_move<0x111, 0xF>(X(0), x);
+  x += dpp_move<0x112, 0xF>(X(0), x);
+  x += dpp_move<0x114, 0xF>(X(0), x);
+  x += dpp_move<0x118, 0xF>(X(0), x);
+  x += dpp_move<0x142, 0xA>(X(0), x);
+  x += dpp_move<0x143, 0xC>(X(0), x);
+  return lane_value(x, 63);
 }
 template <int NT>
 __device__ __forceinline__ float block_max(float x, float* sh) {
@@ -260,34 +295,56 @@ __device__ __forceinline__ float sum_of(const float (&x)[N]) {
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// A row of V elements over NT threads, NV pieces of 16 bytes a thread at a
-// time: piece i is element N i .. N i + N - 1, and the V mod N elements behind
-// the last whole piece go one to each of the first threads.  With KEEP the row
-// is one such chunk and stays in registers between the sweeps; without, every
-// sweep reads it again.
+// How a row lies in 16-byte pieces: `head` elements up to the first 16-byte
+// boundary, `whole` pieces, and the elements behind them (a wave's unaligned
+// 16-byte accesses cost 13 % more with the gradient and 25 % more without at
+// 4096 x 50265 bf16).  The elements at both ends go one to a thread: the head
+// to threads 0 .. N - 1, the tail to N .. 2 N - 1.
+template <class T>
+struct Cut {
+  static constexpr int N = Piece<T>::N;
+  int head, whole;
+  __device__ __forceinline__ Cut(const T* p, int V) {
+    const int over = (int)(reinterpret_cast<uintptr_t>(p) & 15) / (int)sizeof(T);
+    head = over ? min(N - over, V) : 0;
+    whole = (V - head) / N;
+  }
+  // the end element of a thread, -1 if it has none
+  __device__ __forceinline__ int end(int tid, int V) const {
+    if (tid < N) return tid < head ? tid : -1;
+    const int j = head + whole * N + tid - N;
+    return tid < 2 * N && j < V ? j : -1;
+  }
+};
+
+// A row of V elements over NT threads, NV pieces a thread at a time.  With
+// KEEP the row is one such chunk and stays in registers between the sweeps;
+// without, every sweep reads it again.
 template <class T, int NT, int NV, bool KEEP>
 struct RowRegs {
   static constexpr int N = Piece<T>::N;
   const T* z;
-  int V, whole, tid;
+  int head, whole, tid, at;      // at: the thread's end element, -1 if none
   u32x4 raw[NV];
-  float tail;
+  float end;
 
   __device__ __forceinline__ void load(int base) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int i = base + v * NT + tid;
       raw[v] = piece_none<T>();
-      if (i < whole) raw[v] = ld_piece(z + (int64_t)i * N);
+      if (i < whole) raw[v] = ld_piece(z + head + (int64_t)i * N);
     }
   }
-  __device__ __forceinline__ void open(const T* p, int vocab, int thread) {
+  __device__ __forceinline__ void open(const T* p, int V, int thread) {
+    const Cut<T> cut(p, V);
     z = p;
-    V = vocab;
     tid = thread;
-    whole = vocab / N;
-    tail = -INFINITY;
-    if (tid < V - whole * N) tail = load_z(z + (int64_t)whole * N + tid);
+    head = cut.head;
+    whole = cut.whole;
+    at = cut.end(tid, V);
+    end = -INFINITY;
+    if (at >= 0) end = load_z(z + at);
     if constexpr (KEEP) load(0);
   }
   // Makes the next use of the pieces unpack them anew: an unpacked row takes
@@ -313,11 +370,12 @@ struct RowRegs {
 
 // writes zeros over a row
 template <class T, int NT>
-__device__ __forceinline__ void row_zero(T* dz, int V) {
+__device__ __forceinline__ void row_zero(T* dz, int V, int tid) {
   constexpr int N = Piece<T>::N;
-  const int whole = V / N;
-  for (int i = threadIdx.x; i < whole; i += NT) st_piece(dz + (int64_t)i * N, u32x4{0u, 0u, 0u, 0u});
-  if ((int)threadIdx.x < V - whole * N) store_z(dz + (int64_t)whole * N + threadIdx.x, 0.f);
+  const Cut<T> cut(dz, V);
+  for (int i = tid; i < cut.whole; i += NT) st_piece(dz + cut.head + (int64_t)i * N, u32x4{0u, 0u, 0u, 0u});
+  const int at = cut.end(tid, V);
+  if (at >= 0) store_z(dz + at, 0.f);
 }
 
 // ---------------------------------------------------------------------------

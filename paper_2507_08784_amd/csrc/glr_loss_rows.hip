@@ -12,7 +12,8 @@ struct RowIn {
   float zy, coef, old, adv, ref;
   double weight;      // policy: of the row
 };
-__device__ __forceinline__ RowIn row_in(const Rows& r, const Terms& a, const RowPos& p, int seq, float zy) {
+__device__ __forceinline__ RowIn row_in(const Rows& r, const Terms& a, const RowPos& p, int seq, float zy,
+                                      int counted) {
   RowIn x = {};
   x.zy = zy;
   if (a.op == OP_LOGP) {
@@ -24,9 +25,14 @@ __device__ __forceinline__ RowIn row_in(const Rows& r, const Terms& a, const Row
   if (a.ref.p) x.ref = ld_f(a.ref, p);
   double n = a.denom;
   if (a.by_seq) n = (double)a.seqs.n * max(a.count[seq], 1);
-  else if (n == 0.0) n = max(a.count ? *a.count : count_rows(r, a.seqs), 1);
+  else if (n == 0.0) n = max(a.count ? *a.count : counted, 1);
   x.weight = 1.0 / n;
   return x;
+}
+
+// the rows trained on, where the wave counts them itself
+__device__ __forceinline__ int self_count(const Rows& r, const Terms& a) {
+  return a.op == OP_POLICY && !a.by_seq && a.denom == 0.0 && !a.count ? count_rows(r, a.seqs) : 0;
 }
 
 // stores the row's terms and returns g = d loss / d lp times grad_scale / T
@@ -78,11 +84,44 @@ __device__ __forceinline__ bool row_live(const Rows& r, const Seqs& q, const Row
   return seq >= 0;
 }
 
+// a thread's maximum and its sum of 2^((x - maximum) c) (0 where all are -inf)
+template <class T, int NT, int NV, bool KEEP>
+__device__ __forceinline__ void thread_sums(RowRegs<T, NT, NV, KEEP>& row, float c, float& mt, float& st) {
+  constexpr int N = Piece<T>::N;
+  mt = row.end;
+  st = mt == -INFINITY ? 0.f : exp2_of((row.end - mt) * c);
+  row.chunks([&](int) {
+    float top = mt;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float x[N];
+      unpack<T>(row.raw[v], x);
+#pragma unroll
+      for (int k = 0; k < N; ++k) top = fmaxf(top, x[k]);
+      piece_end(top);
+    }
+    const float base = top == -INFINITY ? 0.f : top;
+    st *= exp2_of((mt - base) * c);     // (mt = -inf: st is 0, and stays)
+    mt = top;
+    row.repack();
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float x[N];
+      unpack<T>(row.raw[v], x);
+#pragma unroll
+      for (int k = 0; k < N; ++k) x[k] = exp2_of((x[k] - base) * c);
+      st += sum_of(x);
+      piece_end(st);
+    }
+  });
+}
+
 // a sweep of gradient elements: f e_j, and g more at the target
 template <class T, int NT, int NV, bool KEEP>
 __device__ __forceinline__ void write_grad(RowRegs<T, NT, NV, KEEP>& row, T* dz, float c, float m, float f, float g, int y) {
   constexpr int N = Piece<T>::N;
-  const int iy = y / N, ky = y % N;
+  const int py = y - row.head;          // the target's place among the pieces
+  const int iy = py >= 0 ? py / N : -1, ky = py % N;
   row.chunks([&](int first) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -95,12 +134,11 @@ __device__ __forceinline__ void write_grad(RowRegs<T, NT, NV, KEEP>& row, T* dz,
 #pragma unroll
         for (int k = 0; k < N; ++k) x[k] += k == ky ? g : 0.f;
       }
-      if (i < row.whole) st_piece(dz + (int64_t)i * N, pack<T>(x));
+      if (i < row.whole) st_piece(dz + row.head + (int64_t)i * N, pack<T>(x));
       piece_end();
     }
   });
-  const int at = row.whole * N + row.tid;
-  if (at < row.V) store_z(dz + at, f * exp2_of((row.tail - m) * c) + (at == y ? g : 0.f));
+  if (row.at >= 0) store_z(dz + row.at, f * exp2_of((row.end - m) * c) + (row.at == y ? g : 0.f));
 }
 
 // A workgroup a row: the first waves have the row, the last its terms (what they
@@ -109,7 +147,7 @@ __device__ __forceinline__ void write_grad(RowRegs<T, NT, NV, KEEP>& row, T* dz,
 // sum over the pieces it has; one exchange makes the row's.
 template <class T, int NT, int NV, bool KEEP>
 __global__ void __launch_bounds__(NT + 64) k_loss_row(Rows r, Terms a) {
-  constexpr int N = Piece<T>::N, NW = NT / 64;
+  constexpr int NW = NT / 64;
   __shared__ float m_s[NW], s_s[NW];
   __shared__ float f_s[3];
   const RowPos p = row_pos(r, blockIdx.x);
@@ -118,7 +156,7 @@ __global__ void __launch_bounds__(NT + 64) k_loss_row(Rows r, Terms a) {
   T* dz = r.dz.p ? static_cast<T*>(const_cast<void*>(r.dz.p)) + p.of(r.dz) : nullptr;
   if (!live) {
     if (threadIdx.x == 0) row_masked(r, a, p);
-    if (dz) row_zero<T, NT + 64>(dz, r.V);
+    if (dz) row_zero<T, NT + 64>(dz, r.V, threadIdx.x);
     return;
   }
   const T* z = static_cast<const T*>(r.z.p) + p.of(r.z);
@@ -127,31 +165,8 @@ __global__ void __launch_bounds__(NT + 64) k_loss_row(Rows r, Terms a) {
   if (wave < NW) {
     RowRegs<T, NT, NV, KEEP> row;
     row.open(z, r.V, threadIdx.x);
-    float mt = row.tail, st = mt == -INFINITY ? 0.f : exp2_of((row.tail - mt) * r.c);
-    row.chunks([&](int) {
-      float top = mt;
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        float x[N];
-        unpack<T>(row.raw[v], x);
-#pragma unroll
-        for (int k = 0; k < N; ++k) top = fmaxf(top, x[k]);
-        piece_end(top);
-      }
-      const float base = top == -INFINITY ? 0.f : top;
-      st *= exp2_of((mt - base) * r.c);     // (mt = -inf: st is 0, and stays)
-      mt = top;
-      row.repack();
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        float x[N];
-        unpack<T>(row.raw[v], x);
-#pragma unroll
-        for (int k = 0; k < N; ++k) x[k] = exp2_of((x[k] - base) * r.c);
-        st += sum_of(x);
-        piece_end(st);
-      }
-    });
+    float mt, st;
+    thread_sums(row, r.c, mt, st);
     const float mw = wave_max(mt);
     const float sw = wave_sum(mt == -INFINITY ? st : st * exp2_of((mt - mw) * r.c));
     if ((threadIdx.x & 63) == 0) {
@@ -165,7 +180,7 @@ __global__ void __launch_bounds__(NT + 64) k_loss_row(Rows r, Terms a) {
     return;
   }
   const float nan = __builtin_nanf("");
-  const RowIn x = row_in(r, a, p, seq, y >= 0 ? load_z(z + y) : nan);
+  const RowIn x = row_in(r, a, p, seq, y >= 0 ? load_z(z + y) : nan, self_count(r, a));
   __syncthreads();
   const int lane = threadIdx.x & 63;
   const float mw = lane < NW ? m_s[lane] : -INFINITY;
@@ -180,6 +195,60 @@ __global__ void __launch_bounds__(NT + 64) k_loss_row(Rows r, Terms a) {
   if (dz) __syncthreads();
 }
 
+// Short rows: a wave has R rows in its registers, lane i the terms of row i.
+// No barrier and no wave beside it: at 60000 x 300 the workgroup a row above
+// is bound by the latency of its terms with 16 rows a CU on their way.
+template <class T, int NV, int R>
+__global__ void __launch_bounds__(kLT) k_loss_wave(Rows r, Terms a) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const uint64_t first = ((uint64_t)blockIdx.x * (kLT / 64) + wave) * R;
+  if (first >= r.rows) return;
+  const bool mine = lane < R && first + lane < r.rows;      // lane: its row
+  const RowPos p = row_pos(r, (uint32_t)first + (mine ? lane : 0));
+  int y, seq;
+  const bool live = row_live(r, a.seqs, p, y, seq) && mine;
+  const T* z = static_cast<const T*>(r.z.p) + p.of(r.z);
+  T* dz = r.dz.p ? static_cast<T*>(const_cast<void*>(r.dz.p)) + p.of(r.dz) : nullptr;
+  RowRegs<T, 64, NV, true> row[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    row[i].open(lane_value(z, i), lane_value((int)live, i) ? r.V : 0, lane);
+  const float nan = __builtin_nanf("");
+  const int counted = self_count(r, a);
+  RowIn x = {};
+  if (live) x = row_in(r, a, p, seq, y >= 0 ? load_z(z + y) : nan, counted);
+  float m = 0.f, s = 1.f;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    float mt, st;
+    thread_sums(row[i], r.c, mt, st);
+    const float mi = wave_max(mt), si = wave_sum(mt == -INFINITY ? st : st * exp2_of((mt - mi) * r.c));
+    if (lane == i) {
+      m = mi;
+      s = mi == -INFINITY ? nan : si;
+    }
+  }
+  float f = 0.f, g = 0.f;
+  if (live) {
+    const double d = row_terms(r, a, p, x, m, s);
+    f = y >= 0 ? (float)(-d / (double)s) : nan;
+    g = (float)d;
+  } else if (mine) {
+    row_masked(r, a, p);
+  }
+  if (!r.dz.p) return;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    if (!lane_value((int)mine, i)) break;
+    T* to = lane_value(dz, i);
+    if (lane_value((int)live, i))
+      write_grad(row[i], to, r.c, lane_value(m, i), lane_value(f, i), lane_value(g, i), lane_value(y, i));
+    else
+      row_zero<T, 64>(to, r.V, lane);
+  }
+}
+
 // The gradient from the row's m and s of an earlier call: one sweep.
 template <class T, int NT, int NV>
 __global__ void __launch_bounds__(NT) k_loss_grad(Rows r, Terms a) {
@@ -187,7 +256,7 @@ __global__ void __launch_bounds__(NT) k_loss_grad(Rows r, Terms a) {
   int y, seq;
   const bool live = row_live(r, a.seqs, p, y, seq);
   T* dz = static_cast<T*>(const_cast<void*>(r.dz.p)) + p.of(r.dz);
-  if (!live) return row_zero<T, NT>(dz, r.V);
+  if (!live) return row_zero<T, NT>(dz, r.V, threadIdx.x);
   const float m = a.stats[2 * (int64_t)p.t], s = a.stats[2 * (int64_t)p.t + 1];
   const double g = (double)(a.seq_coef ? a.seq_coef[seq] : ld_f(a.coef, p)) * r.gscale;
   RowRegs<T, NT, NV, false> row;
@@ -198,6 +267,13 @@ __global__ void __launch_bounds__(NT) k_loss_grad(Rows r, Terms a) {
 template <class T, int NT, int NV, bool KEEP>
 void row(const Rows& r, const Terms& a, void* stream) {
   launch("loss rows", k_loss_row<T, NT, NV, KEEP>, r.rows, NT + 64, 0, stream, r, a);
+}
+template <class T, int NV, int R>
+void waves(const Rows& r, const Terms& a, void* stream) {
+  // spread over the chip before rows share a wave
+  if (R > 1 && r.rows <= 8192) return waves<T, NV, 1>(r, a, stream);
+  constexpr unsigned per = kLT / 64 * R;
+  launch("loss rows of a wave", k_loss_wave<T, NV, R>, (r.rows + per - 1) / per, kLT, 0, stream, r, a);
 }
 template <class T, int NT, int NV>
 void grad(const Rows& r, const Terms& a, void* stream) {
@@ -212,13 +288,14 @@ void rows_of(const Rows& r, const Terms& a, void* stream) {
     if (n <= 2048) return grad<T, 256, 4>(r, a, stream);
     return grad<T, 1024, 4>(r, a, stream);
   }
+  if (n <= 64) return waves<T, 1, 8>(r, a, stream);
+  if (n <= 128) return waves<T, 2, 4>(r, a, stream);
+  if (n <= 256) return waves<T, 4, 2>(r, a, stream);
+  if (n <= 512) return waves<T, 8, 1>(r, a, stream);
   if (!r.dz.p) {
-    if (n <= 256) return row<T, 64, 4, false>(r, a, stream);
     if (n <= 1024 || r.rows >= 1024) return row<T, 192, 4, false>(r, a, stream);
     return row<T, 960, 4, false>(r, a, stream);
   }
-  if (n <= 128) return row<T, 64, 2, true>(r, a, stream);
-  if (n <= 256) return row<T, 64, 4, true>(r, a, stream);
   if (n <= 768) return row<T, 192, 4, true>(r, a, stream);
   if (n <= 1792) return row<T, 448, 4, true>(r, a, stream);
   if (n <= 4032) return row<T, 448, 9, true>(r, a, stream);
