@@ -319,8 +319,9 @@ void rows_of(const Rows& r, const Teach& q, void* stream) {
   if (n <= 768) return go<T, REST, TWO, 192, 4, true>(r, q, stream);
   if (n <= 1792) return go<T, REST, TWO, 448, 4, true>(r, q, stream);
   if (n <= 4032) return go<T, REST, TWO, 448, 9, true>(r, q, stream);
-  if (n <= 6720) return go<T, REST, TWO, 960, 7, true>(r, q, stream);
-  if (n <= 9600) return go<T, REST, TWO, 960, 10, true>(r, q, stream);
+  if (n <= 5632) return go<T, REST, TWO, 704, 8, true>(r, q, stream);
+  if (n <= 7040) return go<T, REST, TWO, 704, 10, true>(r, q, stream);
+  if (n <= 9152) return go<T, REST, TWO, 704, 13, true>(r, q, stream);
   if (n <= 13440) return go<T, REST, TWO, 960, 14, true>(r, q, stream);
   if (n <= 16320) return go<T, REST, TWO, 960, 17, true>(r, q, stream);
   return go<T, REST, TWO, 960, 8, false>(r, q, stream);

@@ -107,6 +107,7 @@ enum { OP_LOGP, OP_POLICY, OP_COEF };
 
 struct Terms {
   int32_t op;
+  int32_t again;             // the logits are read again right after
   // LOGP: logps, stats, weights; COEF: stats and coef (per row) or seq_coef (per sequence)
   float* logps;
   float* stats;
@@ -236,8 +237,11 @@ __device__ __forceinline__ u32x4 piece_none() {
   constexpr uint32_t x = Piece<T>::kNone;
   return u32x4{x, x, x, x};
 }
-template <class T>
+// STAY: the piece is read again soon and may stay in the memory-side cache,
+// which non-temporal loads pass by
+template <bool STAY, class T>
 __device__ __forceinline__ u32x4 ld_piece(const T* p) {
+  if constexpr (STAY) return *reinterpret_cast<const u32x4_any*>(p);
   return __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p));
 }
 template <class T>
@@ -320,7 +324,7 @@ struct Cut {
 // A row of V elements over NT threads, NV pieces a thread at a time.  With
 // KEEP the row is one such chunk and stays in registers between the sweeps;
 // without, every sweep reads it again.
-template <class T, int NT, int NV, bool KEEP>
+template <class T, int NT, int NV, bool KEEP, bool STAY = false>
 struct RowRegs {
   static constexpr int N = Piece<T>::N;
   const T* z;
@@ -333,7 +337,7 @@ struct RowRegs {
     for (int v = 0; v < NV; ++v) {
       const int i = base + v * NT + tid;
       raw[v] = piece_none<T>();
-      if (i < whole) raw[v] = ld_piece(z + head + (int64_t)i * N);
+      if (i < whole) raw[v] = ld_piece<STAY>(z + head + (int64_t)i * N);
     }
   }
   __device__ __forceinline__ void open(const T* p, int V, int thread) {

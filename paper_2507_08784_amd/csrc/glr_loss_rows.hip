@@ -85,8 +85,8 @@ __device__ __forceinline__ bool row_live(const Rows& r, const Seqs& q, const Row
 }
 
 // a thread's maximum and its sum of 2^((x - maximum) c) (0 where all are -inf)
-template <class T, int NT, int NV, bool KEEP>
-__device__ __forceinline__ void thread_sums(RowRegs<T, NT, NV, KEEP>& row, float c, float& mt, float& st) {
+template <class T, int NT, int NV, bool KEEP, bool STAY>
+__device__ __forceinline__ void thread_sums(RowRegs<T, NT, NV, KEEP, STAY>& row, float c, float& mt, float& st) {
   constexpr int N = Piece<T>::N;
   mt = row.end;
   st = mt == -INFINITY ? 0.f : exp2_of((row.end - mt) * c);
@@ -117,8 +117,8 @@ __device__ __forceinline__ void thread_sums(RowRegs<T, NT, NV, KEEP>& row, float
 }
 
 // a sweep of gradient elements: f e_j, and g more at the target
-template <class T, int NT, int NV, bool KEEP>
-__device__ __forceinline__ void write_grad(RowRegs<T, NT, NV, KEEP>& row, T* dz, float c, float m, float f, float g, int y) {
+template <class T, int NT, int NV, bool KEEP, bool STAY>
+__device__ __forceinline__ void write_grad(RowRegs<T, NT, NV, KEEP, STAY>& row, T* dz, float c, float m, float f, float g, int y) {
   constexpr int N = Piece<T>::N;
   const int py = y - row.head;          // the target's place among the pieces
   const int iy = py >= 0 ? py / N : -1, ky = py % N;
@@ -145,7 +145,7 @@ __device__ __forceinline__ void write_grad(RowRegs<T, NT, NV, KEEP>& row, T* dz,
 // need is loaded while the row is on its way, and their fp64 takes no
 // registers beside a row's).  Each thread keeps its own running maximum and
 // sum over the pieces it has; one exchange makes the row's.
-template <class T, int NT, int NV, bool KEEP>
+template <class T, int NT, int NV, bool KEEP, bool STAY>
 __global__ void __launch_bounds__(NT + 64) k_loss_row(Rows r, Terms a) {
   constexpr int NW = NT / 64;
   __shared__ float m_s[NW], s_s[NW];
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(NT + 64) k_loss_row(Rows r, Terms a) {
   // (a scalar: the two parts meet at the same number of barriers, wave by wave)
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   if (wave < NW) {
-    RowRegs<T, NT, NV, KEEP> row;
+    RowRegs<T, NT, NV, KEEP, STAY> row;
     row.open(z, r.V, threadIdx.x);
     float mt, st;
     thread_sums(row, r.c, mt, st);
@@ -249,10 +249,11 @@ __global__ void __launch_bounds__(kLT) k_loss_wave(Rows r, Terms a) {
   }
 }
 
-// The gradient from the row's m and s of an earlier call: one sweep.
+// The gradient from the row's m and s of an earlier call: one sweep, from the
+// last row to the first (the ones read last are those still in a cache).
 template <class T, int NT, int NV>
 __global__ void __launch_bounds__(NT) k_loss_grad(Rows r, Terms a) {
-  const RowPos p = row_pos(r, blockIdx.x);
+  const RowPos p = row_pos(r, r.rows - 1 - blockIdx.x);
   int y, seq;
   const bool live = row_live(r, a.seqs, p, y, seq);
   T* dz = static_cast<T*>(const_cast<void*>(r.dz.p)) + p.of(r.dz);
@@ -264,9 +265,9 @@ __global__ void __launch_bounds__(NT) k_loss_grad(Rows r, Terms a) {
   write_grad(row, dz, r.c, m, y >= 0 ? (float)(-g / (double)s) : __builtin_nanf(""), (float)g, y);
 }
 
-template <class T, int NT, int NV, bool KEEP>
+template <class T, int NT, int NV, bool KEEP, bool STAY = false>
 void row(const Rows& r, const Terms& a, void* stream) {
-  launch("loss rows", k_loss_row<T, NT, NV, KEEP>, r.rows, NT + 64, 0, stream, r, a);
+  launch("loss rows", k_loss_row<T, NT, NV, KEEP, STAY>, r.rows, NT + 64, 0, stream, r, a);
 }
 template <class T, int NV, int R>
 void waves(const Rows& r, const Terms& a, void* stream) {
@@ -278,6 +279,22 @@ void waves(const Rows& r, const Terms& a, void* stream) {
 template <class T, int NT, int NV>
 void grad(const Rows& r, const Terms& a, void* stream) {
   launch("loss gradient rows", k_loss_grad<T, NT, NV>, r.rows, NT, 0, stream, r, a);
+}
+
+// A preference loss reads its logits twice.  The last 256 MB of the first
+// reading can be in the memory-side cache at the second if its loads are not
+// non-temporal (8192 x 32000 bf16, a third of it trained on: 180 -> 154 us;
+// 3295 x 128000 fp16, 397 -> 385), which costs such a reading about 10 %: above
+// 2 GiB more than it saves.
+constexpr int64_t kStayBytes = (int64_t)2 << 30;
+
+// no gradient: the row is read once, in chunks
+template <class T, bool STAY>
+void sums_of(const Rows& r, const Terms& a, void* stream) {
+  const int n = r.V / Piece<T>::N;
+  if (n <= 1024 || (n <= 4096 && r.rows >= 1024)) return row<T, 192, 4, false, STAY>(r, a, stream);
+  if (r.rows >= 1024) return row<T, 448, 4, false, STAY>(r, a, stream);
+  return row<T, 960, 4, false, STAY>(r, a, stream);
 }
 
 template <class T>
@@ -293,14 +310,15 @@ void rows_of(const Rows& r, const Terms& a, void* stream) {
   if (n <= 256) return waves<T, 4, 2>(r, a, stream);
   if (n <= 512) return waves<T, 8, 1>(r, a, stream);
   if (!r.dz.p) {
-    if (n <= 1024 || r.rows >= 1024) return row<T, 192, 4, false>(r, a, stream);
-    return row<T, 960, 4, false>(r, a, stream);
+    if (a.again && (int64_t)r.rows * r.V * (int64_t)sizeof(T) <= kStayBytes) return sums_of<T, true>(r, a, stream);
+    return sums_of<T, false>(r, a, stream);
   }
   if (n <= 768) return row<T, 192, 4, true>(r, a, stream);
   if (n <= 1792) return row<T, 448, 4, true>(r, a, stream);
   if (n <= 4032) return row<T, 448, 9, true>(r, a, stream);
-  if (n <= 6720) return row<T, 960, 7, true>(r, a, stream);
-  if (n <= 9600) return row<T, 960, 10, true>(r, a, stream);
+  if (n <= 5632) return row<T, 704, 8, true>(r, a, stream);
+  if (n <= 7040) return row<T, 704, 10, true>(r, a, stream);
+  if (n <= 9152) return row<T, 704, 13, true>(r, a, stream);
   if (n <= 13440) return row<T, 960, 14, true>(r, a, stream);
   if (n <= 16320) return row<T, 960, 17, true>(r, a, stream);
   if (n <= 20160) return row<T, 960, 21, true>(r, a, stream);

@@ -318,6 +318,7 @@ glr_status glr_preference_loss(const glr_loss_rows* rows, const glr_pref_args* x
     a.seqs = q;
     a.logps = reinterpret_cast<float*>(ws + s.lp);
     a.stats = r.dz.p ? reinterpret_cast<float*>(ws + s.stats) : nullptr;
+    a.again = r.dz.p != nullptr;
     Rows f = r;
     f.dz.p = nullptr;
     loss_rows(rows->dtype, f, a, stream);
