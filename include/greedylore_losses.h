@@ -44,7 +44,10 @@
  * buffer; the calls only enqueue, on `stream`, and may be captured into a HIP
  * graph; they keep nothing between calls.  d_ws is scratch of at least
  * glr_loss_workspace_bytes bytes, 16-byte aligned, in use until the call's
- * work has run.  Argument errors are found before anything is enqueued; the
+ * work has run; its first 16 bytes must be zero then, and the call leaves
+ * them zero (waves that finish count themselves there): scratch that was
+ * cleared once serves any number of calls on one stream, of any of the losses,
+ * and calls that may run at the same time need scratch of their own.  Argument errors are found before anything is enqueued; the
  * text is glr_last_error(NULL).
  */
 #ifndef GREEDYLORE_LOSSES_H

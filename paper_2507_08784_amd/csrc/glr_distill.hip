@@ -42,6 +42,14 @@ struct Coefs {
   float m, out, in, one, soft, hard;
 };
 
+// A wave has stored its row's loss: the last of the call's makes the total.
+__device__ __forceinline__ void row_done(const Rows& r, const Teach& q) {
+  if (!q.sync || !last_to_arrive(q.sync, r.rows)) return;
+  const double x = total_of(q.losses, r.rows);
+  const double n = q.denom > 0.0 ? q.denom : (double)max(count_rows(r, Seqs{}), 1);
+  if ((threadIdx.x & 63) == 0) *q.loss = (float)(x / n);
+}
+
 // A workgroup a row: the first waves have the row, the last has the teacher's list
 // (its loads, exponentials and logarithms run while the row is on its way, and
 // its fp64 takes no registers beside a row's).  The list's tokens are marked
@@ -64,14 +72,15 @@ __global__ void __launch_bounds__(NT + 64) k_distill_row(Rows r, Teach q) {
   int y;
   const bool live = row_target(r, p, y);
   T* dz = r.dz.p ? static_cast<T*>(const_cast<void*>(r.dz.p)) + p.of(r.dz) : nullptr;
+  // (a scalar: the two parts meet at the same number of barriers, wave by wave)
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   if (!live) {
-    if (threadIdx.x == 0) q.losses[p.t] = 0.f;
+    if (threadIdx.x == 0) put_shared(q.losses + p.t, 0.f);
     if (dz) row_zero<T, NT + 64>(dz, r.V, threadIdx.x);
+    if (wave == 0) row_done(r, q);
     return;
   }
   const T* z = static_cast<const T*>(r.z.p) + p.of(r.z);
-  // (a scalar: the two parts meet at the same number of barriers, wave by wave)
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   if (wave < NW) {
     // ---- the row
     RowRegs<T, NT, NV, KEEP> row;
@@ -281,8 +290,9 @@ __global__ void __launch_bounds__(NT + 64) k_distill_row(Rows r, Teach q) {
     double loss = (1.0 - q.hard) * kl / (r.inv_t * r.inv_t);
     if (s != s) loss = s;
     if (q.hard > 0.0) loss -= q.hard * ((double)zy - (double)m - log(s1));
-    q.losses[p.t] = bad ? nan : (float)loss;
+    put_shared(q.losses + p.t, bad ? nan : (float)loss);
   }
+  row_done(r, q);
   if (!dz) return;
   __syncthreads();
   const Coefs a = co;

@@ -22,7 +22,11 @@ typedef _Float16 f16_t;
 
 constexpr int kLT = 256;                        // threads of the small kernels
 constexpr int kMaxTop = 1024;
-constexpr uint32_t kSelfCount = 1024;           // rows that every row's own wave counts
+// A call of up to kSelfCount rows is one launch (two with a preference's
+// gradient): every row's wave counts the rows trained on itself (16 loads a
+// lane, beside the row's), and the last wave to arrive makes the totals.
+constexpr uint32_t kSelfCount = 1024;
+constexpr int32_t kSelfSeqs = 64;               // sequences of such a preference loss
 constexpr int64_t kMaxLossVocab = (int64_t)1 << 28;
 constexpr int64_t kMaxDistillVocab = (int64_t)1 << 19;   // the list's bitmap stays within 64 KB of LDS
 constexpr double kRestFloor = 1.0 / (1 << 20);
@@ -105,6 +109,21 @@ __device__ __forceinline__ bool row_target(const Rows& r, const RowPos& p, int& 
 
 enum { OP_LOGP, OP_POLICY, OP_COEF };
 
+// The pairs of a preference loss.
+struct Pairs {
+  Seqs seqs;
+  int kind, average;
+  double beta, smooth;
+  const float* ref;
+  float* loss;
+  float* logps;
+  float* rewards;
+  const float* lp;     // of the rows
+  float* coef;         // d loss / d lp of a sequence's rows
+  float* part;         // a pair's loss
+  uint32_t* sync;
+};
+
 struct Terms {
   int32_t op;
   int32_t again;             // the logits are read again right after
@@ -121,6 +140,11 @@ struct Terms {
   int by_seq;                // weight 1 / (seqs * count[sequence])
   const int* count;
   float* part;               // 3 x rows: w term, w kl, w clipped
+  float* out[3];             // their sums
+  // The last wave to arrive makes the call's totals (NULL: a launch of their
+  // own does): of the policy's parts, or the pairs of a preference loss.
+  uint32_t* sync;
+  Pairs pairs;
 };
 
 // ---------------------------------------------------------------------------
@@ -205,18 +229,88 @@ struct Teach {
   double hard, denom;
   const int* count;    // NULL (and denom 0): as counted
   float* losses;       // a row's loss
+  float* loss;
+  uint32_t* sync;      // the last wave to arrive makes the total (NULL: a launch of its own)
 };
 
-// The rows trained on, by one wave: up to kSelfCount rows it takes 16 loads a
-// lane beside the row's; more are counted by a launch of their own.
-__device__ __forceinline__ int count_rows(const Rows& r, const Seqs& q) {
-  const uint32_t lo = q.cu ? seq_off(q, 0, r.rows) : 0, hi = q.cu ? seq_off(q, q.n, r.rows) : r.rows;
+// the rows of sequence i
+__device__ __forceinline__ void seq_span(const Rows& r, const Seqs& q, int64_t i, uint32_t& lo, uint32_t& hi) {
+  lo = q.cu ? seq_off(q, i, r.rows) : (uint32_t)i * r.steps;
+  hi = q.cu ? seq_off(q, i + 1, r.rows) : lo + r.steps;
+}
+// the rows trained on in [lo, hi), by one wave
+__device__ __forceinline__ int count_span(const Rows& r, uint32_t lo, uint32_t hi) {
   int n = 0;
-  for (uint32_t t = lo + (threadIdx.x & 63); t < hi; t += 64) {
+  for (uint64_t t = (uint64_t)lo + (threadIdx.x & 63); t < hi; t += 64) {
     int y;
-    n += row_target(r, row_pos(r, t), y);
+    n += row_target(r, row_pos(r, (uint32_t)t), y);
   }
   return wave_sum(n);
+}
+// of everything
+__device__ __forceinline__ int count_rows(const Rows& r, const Seqs& q) {
+  return count_span(r, q.cu ? seq_off(q, 0, r.rows) : 0, q.cu ? seq_off(q, q.n, r.rows) : r.rows);
+}
+
+// What the last wave of a call reads is stored and loaded by agent-scope
+// atomics, which meet where the caches of the chip's dies do, and the wait
+// puts a wave's stores before its arrival (a fence instead would write back
+// the die's whole cache, gradients and all).  The word is 0 before and after.
+__device__ __forceinline__ void put_shared(float* p, float x) {
+  __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float get_shared(const float* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// by a whole wave, behind its stores
+__device__ __forceinline__ bool last_to_arrive(uint32_t* word, uint32_t expected) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  uint32_t n = 0;
+  if ((threadIdx.x & 63) == 0) n = __hip_atomic_fetch_add(word, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  n = __builtin_amdgcn_readfirstlane(n);
+  asm volatile("" ::: "memory");
+  if (n != expected - 1) return false;
+  if ((threadIdx.x & 63) == 0) __hip_atomic_store(word, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return true;
+}
+// the sum of n parts, by one wave
+__device__ __forceinline__ double total_of(const float* part, uint32_t n) {
+  double x = 0.0;
+  for (uint32_t i = threadIdx.x & 63; i < n; i += 64) x += get_shared(part + i);
+  return wave_sum(x);
+}
+
+// a pair's loss and what its sequences' rows get, from the sums of their log-probabilities
+__device__ __forceinline__ void pair_terms(const Pairs& q, int i, double L0, int n0, double L1, int n1) {
+  const int half = q.seqs.n >> 1, j = i + half;
+  n0 = max(n0, 1);
+  n1 = max(n1, 1);
+  L0 /= n0;
+  L1 /= n1;
+  const double rc = L0 - (double)q.ref[i], rr = L1 - (double)q.ref[j];
+  const double delta = rc - rr, h = q.beta * delta;
+  double loss, slope;
+  if (q.kind == GLR_PREF_SIGMOID) {
+    const double soft = log1p(exp(-fabs(h)));
+    const double neg = soft + (h < 0.0 ? -h : 0.0), pos = soft + (h > 0.0 ? h : 0.0);   // -log sigma(h), -log sigma(-h)
+    loss = (1.0 - q.smooth) * neg + q.smooth * pos;
+    slope = q.beta * (q.smooth - 1.0 / (1.0 + exp(h)));
+    if (h != h) loss = h;
+  } else if (q.kind == GLR_PREF_HINGE) {
+    loss = h < 1.0 ? 1.0 - h : h == h ? 0.0 : h;
+    slope = h < 1.0 ? -q.beta : h == h ? 0.0 : h;
+  } else {
+    const double off = delta - 0.5 / q.beta;
+    loss = off * off;
+    slope = 2.0 * off;
+  }
+  q.logps[i] = (float)L0;
+  q.logps[j] = (float)L1;
+  q.rewards[i] = (float)(q.beta * rc);
+  q.rewards[j] = (float)(q.beta * rr);
+  q.coef[i] = (float)(slope / half / n0);
+  q.coef[j] = (float)(-slope / half / n1);
+  put_shared(q.part + i, (float)loss);
 }
 
 // ---------------------------------------------------------------------------

@@ -24,22 +24,26 @@ __device__ __forceinline__ RowIn row_in(const Rows& r, const Terms& a, const Row
   x.adv = ld_f(a.adv, p);
   if (a.ref.p) x.ref = ld_f(a.ref, p);
   double n = a.denom;
-  if (a.by_seq) n = (double)a.seqs.n * max(a.count[seq], 1);
+  if (a.by_seq) n = (double)a.seqs.n * max(a.count ? a.count[seq] : counted, 1);
   else if (n == 0.0) n = max(a.count ? *a.count : counted, 1);
   x.weight = 1.0 / n;
   return x;
 }
 
-// the rows trained on, where the wave counts them itself
-__device__ __forceinline__ int self_count(const Rows& r, const Terms& a) {
-  return a.op == OP_POLICY && !a.by_seq && a.denom == 0.0 && !a.count ? count_rows(r, a.seqs) : 0;
+// the rows that share a row's weight, where the wave counts them itself
+__device__ __forceinline__ int self_count(const Rows& r, const Terms& a, int seq) {
+  if (a.op != OP_POLICY || a.count) return 0;
+  if (!a.by_seq) return a.denom == 0.0 ? count_rows(r, a.seqs) : 0;
+  uint32_t lo, hi;
+  seq_span(r, a.seqs, seq, lo, hi);
+  return count_span(r, lo, hi);
 }
 
 // stores the row's terms and returns g = d loss / d lp times grad_scale / T
 __device__ __forceinline__ double row_terms(const Rows& r, const Terms& a, const RowPos& p, const RowIn& x, float m,
                                             float s) {
   const double lp = ((double)x.zy - (double)m) * r.inv_t - log((double)s);
-  a.logps[p.t] = (float)lp;
+  put_shared(a.logps + p.t, (float)lp);
   if (a.op == OP_LOGP) {
     if (a.stats) {
       a.stats[2 * (int64_t)p.t] = m;
@@ -58,14 +62,14 @@ __device__ __forceinline__ double row_terms(const Rows& r, const Terms& a, const
     term += a.kl * k;
     slope -= a.kl * y;
   }
-  a.part[p.t] = (float)(x.weight * term);
-  a.part[(int64_t)r.rows + p.t] = (float)(x.weight * k);
-  a.part[2 * (int64_t)r.rows + p.t] = cut ? (float)x.weight : 0.f;
+  put_shared(a.part + p.t, (float)(x.weight * term));
+  put_shared(a.part + (int64_t)r.rows + p.t, (float)(x.weight * k));
+  put_shared(a.part + 2 * (int64_t)r.rows + p.t, cut ? (float)x.weight : 0.f);
   return x.weight * slope * r.gscale;
 }
 // what a masked row leaves
 __device__ __forceinline__ void row_masked(const Rows& r, const Terms& a, const RowPos& p) {
-  a.logps[p.t] = 0.f;
+  put_shared(a.logps + p.t, 0.f);
   if (a.op == OP_LOGP) {
     if (a.stats) {
       a.stats[2 * (int64_t)p.t] = 0.f;
@@ -73,7 +77,36 @@ __device__ __forceinline__ void row_masked(const Rows& r, const Terms& a, const 
     }
     return;
   }
-  for (int k = 0; k < 3; ++k) a.part[k * (int64_t)r.rows + p.t] = 0.f;
+  for (int k = 0; k < 3; ++k) put_shared(a.part + k * (int64_t)r.rows + p.t, 0.f);
+}
+
+// A wave has stored its rows' terms: the last of the call's makes the totals.
+__device__ __forceinline__ void row_done(const Rows& r, const Terms& a, uint32_t waves) {
+  if (!a.sync || !last_to_arrive(a.sync, waves)) return;
+  const int lane = threadIdx.x & 63;
+  if (a.op == OP_POLICY) {
+    for (int k = 0; k < 3; ++k) {
+      const double x = total_of(a.part + k * (int64_t)r.rows, r.rows);
+      if (lane == 0) *a.out[k] = (float)x;
+    }
+    return;
+  }
+  const Pairs& q = a.pairs;
+  const int half = q.seqs.n >> 1;
+  for (int i = 0; i < half; ++i) {
+    double L[2];
+    int n[2] = {1, 1};
+    for (int side = 0; side < 2; ++side) {
+      uint32_t lo, hi;
+      seq_span(r, q.seqs, i + side * (int64_t)half, lo, hi);
+      L[side] = total_of(q.lp + lo, hi > lo ? hi - lo : 0);      // (0 where masked)
+      if (q.average) n[side] = count_span(r, lo, hi);
+    }
+    if (lane == 0) pair_terms(q, i, L[0], n[0], L[1], n[1]);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // lane 0's parts
+  const double loss = total_of(q.part, half);
+  if (lane == 0) *q.loss = (float)(loss / half);
 }
 
 // whether a row is trained on; its target and its sequence
@@ -154,14 +187,15 @@ __global__ void __launch_bounds__(NT + 64) k_loss_row(Rows r, Terms a) {
   int y, seq;
   const bool live = row_live(r, a.seqs, p, y, seq);
   T* dz = r.dz.p ? static_cast<T*>(const_cast<void*>(r.dz.p)) + p.of(r.dz) : nullptr;
+  // (a scalar: the two parts meet at the same number of barriers, wave by wave)
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   if (!live) {
     if (threadIdx.x == 0) row_masked(r, a, p);
     if (dz) row_zero<T, NT + 64>(dz, r.V, threadIdx.x);
+    if (wave == 0) row_done(r, a, r.rows);
     return;
   }
   const T* z = static_cast<const T*>(r.z.p) + p.of(r.z);
-  // (a scalar: the two parts meet at the same number of barriers, wave by wave)
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   if (wave < NW) {
     RowRegs<T, NT, NV, KEEP, STAY> row;
     row.open(z, r.V, threadIdx.x);
@@ -180,7 +214,7 @@ __global__ void __launch_bounds__(NT + 64) k_loss_row(Rows r, Terms a) {
     return;
   }
   const float nan = __builtin_nanf("");
-  const RowIn x = row_in(r, a, p, seq, y >= 0 ? load_z(z + y) : nan, self_count(r, a));
+  const RowIn x = row_in(r, a, p, seq, y >= 0 ? load_z(z + y) : nan, self_count(r, a, seq));
   __syncthreads();
   const int lane = threadIdx.x & 63;
   const float mw = lane < NW ? m_s[lane] : -INFINITY;
@@ -193,6 +227,7 @@ __global__ void __launch_bounds__(NT + 64) k_loss_row(Rows r, Terms a) {
     f_s[2] = (float)g;
   }
   if (dz) __syncthreads();
+  row_done(r, a, r.rows);
 }
 
 // Short rows: a wave has R rows in its registers, lane i the terms of row i.
@@ -215,7 +250,8 @@ __global__ void __launch_bounds__(kLT) k_loss_wave(Rows r, Terms a) {
   for (int i = 0; i < R; ++i)
     row[i].open(lane_value(z, i), lane_value((int)live, i) ? r.V : 0, lane);
   const float nan = __builtin_nanf("");
-  const int counted = self_count(r, a);
+  // (R = 1: its row's; several rows of a wave have their counts from a launch)
+  const int counted = self_count(r, a, max(lane_value(seq, 0), 0));
   RowIn x = {};
   if (live) x = row_in(r, a, p, seq, y >= 0 ? load_z(z + y) : nan, counted);
   float m = 0.f, s = 1.f;
@@ -237,16 +273,16 @@ __global__ void __launch_bounds__(kLT) k_loss_wave(Rows r, Terms a) {
   } else if (mine) {
     row_masked(r, a, p);
   }
-  if (!r.dz.p) return;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
-    if (!lane_value((int)mine, i)) break;
+    if (!r.dz.p || !lane_value((int)mine, i)) break;
     T* to = lane_value(dz, i);
     if (lane_value((int)live, i))
       write_grad(row[i], to, r.c, lane_value(m, i), lane_value(f, i), lane_value(g, i), lane_value(y, i));
     else
       row_zero<T, 64>(to, r.V, lane);
   }
+  row_done(r, a, (r.rows + R - 1) / R);
 }
 
 // The gradient from the row's m and s of an earlier call: one sweep, from the

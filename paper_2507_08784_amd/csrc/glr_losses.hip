@@ -23,8 +23,7 @@ __global__ void __launch_bounds__(1024) k_loss_count(Rows r, Seqs q, int by_seq,
   __shared__ int sh[16];
   uint32_t lo = 0, hi = r.rows;
   if (by_seq) {
-    lo = q.cu ? seq_off(q, blockIdx.x, r.rows) : blockIdx.x * r.steps;
-    hi = q.cu ? seq_off(q, (int64_t)blockIdx.x + 1, r.rows) : lo + r.steps;
+    seq_span(r, q, blockIdx.x, lo, hi);
   } else if (q.cu) {
     lo = seq_off(q, 0, r.rows);
     hi = seq_off(q, q.n, r.rows);
@@ -38,69 +37,31 @@ __global__ void __launch_bounds__(1024) k_loss_count(Rows r, Seqs q, int by_seq,
   if (threadIdx.x == 0) count[blockIdx.x] = n;
 }
 
-struct Pairs {
-  Seqs seqs;
-  int kind, average;
-  double beta, smooth;
-  const float* ref;
-  const float* lp;     // of the rows
-  float* logps;
-  float* rewards;
-  float* coef;         // d loss / d lp of a sequence's rows
-  float* part;         // a pair's loss
-};
-
-__global__ void __launch_bounds__(kLT) k_loss_pairs(Rows r, Pairs q) {
-  __shared__ double shd[kLT / 64];
-  __shared__ int shi[kLT / 64];
+// A workgroup a pair; the last one adds the pairs' losses.
+__global__ void __launch_bounds__(1024) k_loss_pairs(Rows r, Pairs q) {
+  __shared__ double shd[16];
+  __shared__ int shi[16];
   const int half = q.seqs.n >> 1;
   double L[2];
   int n[2];
   for (int side = 0; side < 2; ++side) {
-    const int i = (int)blockIdx.x + side * half;
-    const uint32_t lo = q.seqs.cu ? seq_off(q.seqs, i, r.rows) : (uint32_t)i * r.steps;
-    const uint32_t hi = q.seqs.cu ? seq_off(q.seqs, i + 1, r.rows) : lo + r.steps;
+    uint32_t lo, hi;
+    seq_span(r, q.seqs, (int64_t)blockIdx.x + side * (int64_t)half, lo, hi);
     double x = 0.0;
     int c = 0;
-    for (uint64_t t = (uint64_t)lo + threadIdx.x; t < hi; t += kLT) {
+    for (uint64_t t = (uint64_t)lo + threadIdx.x; t < hi; t += 1024) {
       int y;
-      if (row_target(r, row_pos(r, (uint32_t)t), y)) {
-        x += q.lp[t];
-        ++c;
-      }
+      if (q.average) c += row_target(r, row_pos(r, (uint32_t)t), y);
+      x += q.lp[t];                                                    // (0 where masked)
     }
-    L[side] = block_sum<kLT, double>(x, shd);
-    n[side] = q.average ? block_sum<kLT, int>(c, shi) : 1;
-    if (n[side] < 1) n[side] = 1;
-    L[side] /= n[side];
+    L[side] = block_sum<1024, double>(x, shd);
+    n[side] = q.average ? block_sum<1024, int>(c, shi) : 1;
   }
-  if (threadIdx.x) return;
-  const int i = blockIdx.x, j = i + half;
-  const double rc = L[0] - (double)q.ref[i], rr = L[1] - (double)q.ref[j];
-  const double delta = rc - rr, h = q.beta * delta;
-  double loss, slope;
-  if (q.kind == GLR_PREF_SIGMOID) {
-    const double soft = log1p(exp(-fabs(h)));
-    const double neg = soft + (h < 0.0 ? -h : 0.0), pos = soft + (h > 0.0 ? h : 0.0);   // -log sigma(h), -log sigma(-h)
-    loss = (1.0 - q.smooth) * neg + q.smooth * pos;
-    slope = q.beta * (q.smooth - 1.0 / (1.0 + exp(h)));
-    if (h != h) loss = h;
-  } else if (q.kind == GLR_PREF_HINGE) {
-    loss = h < 1.0 ? 1.0 - h : h == h ? 0.0 : h;
-    slope = h < 1.0 ? -q.beta : h == h ? 0.0 : h;
-  } else {
-    const double off = delta - 0.5 / q.beta;
-    loss = off * off;
-    slope = 2.0 * off;
-  }
-  q.logps[i] = (float)L[0];
-  q.logps[j] = (float)L[1];
-  q.rewards[i] = (float)(q.beta * rc);
-  q.rewards[j] = (float)(q.beta * rr);
-  q.part[i] = (float)loss;
-  if (q.coef) {
-    q.coef[i] = (float)(slope / half / n[0]);
-    q.coef[j] = (float)(-slope / half / n[1]);
+  if (threadIdx.x >= 64) return;
+  if (threadIdx.x == 0) pair_terms(q, blockIdx.x, L[0], n[0], L[1], n[1]);
+  if (last_to_arrive(q.sync, gridDim.x)) {
+    const double loss = total_of(q.part, gridDim.x);
+    if (threadIdx.x == 0) *q.loss = (float)(loss / half);
   }
 }
 
@@ -112,7 +73,7 @@ __global__ void __launch_bounds__(1024) k_loss_total(const float* part, Rows r, 
   double x = 0.0;
   for (int64_t i = threadIdx.x; i < r.rows; i += 1024) x += part[blockIdx.x * (int64_t)r.rows + i];
   x = block_sum<1024, double>(x, sh);
-  if (denom == 0.0) denom = max(count ? *count : count_rows(r, Seqs{}), 1);
+  if (denom == 0.0) denom = max(*count, 1);
   if (threadIdx.x == 0) *out = (float)(x / denom);
 }
 
@@ -209,7 +170,7 @@ constexpr size_t up16(size_t x) { return (x + 15) / 16 * 16; }
 
 // scratch of a call, in 16-byte aligned pieces
 struct Scratch {
-  size_t lp = 0, stats = 0, coef = 0, part = 0, count = 0, bytes = 0;
+  size_t sync = 0, lp = 0, stats = 0, coef = 0, part = 0, count = 0, bytes = 0;
   size_t take(size_t n) {
     const size_t at = bytes;
     bytes += up16(n);
@@ -218,6 +179,7 @@ struct Scratch {
 };
 Scratch scratch_of(int op, int64_t rows, int64_t seqs, bool grad) {
   Scratch s;
+  if (op != GLR_LOSS_LOGPROBS) s.sync = s.take(16);
   if (op == GLR_LOSS_PREFERENCE) {
     s.lp = s.take(4 * rows);
     s.stats = s.take(grad ? 8 * rows : 0);
@@ -313,32 +275,33 @@ glr_status glr_preference_loss(const glr_loss_rows* rows, const glr_pref_args* x
     check_out(x->rewards, "rewards");
     const Scratch s = scratch_of(GLR_LOSS_PREFERENCE, r.rows, q.n, r.dz.p != nullptr);
     char* ws = check_ws(s, d_ws, ws_bytes);
+    uint32_t* sync = reinterpret_cast<uint32_t*>(ws + s.sync);
     Terms a = {};
     a.op = OP_LOGP;
     a.seqs = q;
     a.logps = reinterpret_cast<float*>(ws + s.lp);
     a.stats = r.dz.p ? reinterpret_cast<float*>(ws + s.stats) : nullptr;
-    a.again = r.dz.p != nullptr;
-    Rows f = r;
-    f.dz.p = nullptr;
-    loss_rows(rows->dtype, f, a, stream);
-    Pairs b = {};
+    Pairs& b = a.pairs;
     b.seqs = q;
     b.kind = x->kind;
     b.average = x->average;
     b.beta = x->beta;
     b.smooth = x->label_smoothing;
     b.ref = x->ref_logps;
-    b.lp = a.logps;
+    b.loss = x->loss;
     b.logps = x->logps;
     b.rewards = x->rewards;
+    b.lp = a.logps;
     b.coef = reinterpret_cast<float*>(ws + s.coef);
     b.part = reinterpret_cast<float*>(ws + s.part);
-    launch("loss pairs", k_loss_pairs, q.n / 2, kLT, 0, stream, r, b);
-    Rows pairs = r;
-    pairs.rows = (uint32_t)q.n / 2;
-    launch("loss total", k_loss_total, 1, 1024, 0, stream, b.part, pairs, (double)pairs.rows, nullptr, x->loss, nullptr,
-           nullptr);
+    b.sync = sync;
+    const bool few = r.rows > 0 && r.rows <= kSelfCount && q.n <= kSelfSeqs;
+    a.sync = few ? sync : nullptr;
+    a.again = r.dz.p != nullptr;
+    Rows f = r;
+    f.dz.p = nullptr;
+    loss_rows(rows->dtype, f, a, stream);
+    if (!few) launch("loss pairs", k_loss_pairs, q.n / 2, 1024, 0, stream, r, b);
     if (r.dz.p) {
       a.op = OP_COEF;
       a.seq_coef = b.coef;
@@ -390,13 +353,18 @@ glr_status glr_policy_loss(const glr_loss_rows* rows, const glr_policy_args* x, 
     a.denom = x->denominator;
     a.by_seq = by_seq;
     int* count = reinterpret_cast<int*>(ws + s.count);
-    // (no count: each row's own wave counts)
-    const bool counted = by_seq || (a.denom == 0.0 && r.rows > kSelfCount);
+    const bool few = r.rows > 0 && r.rows <= kSelfCount;
+    const bool counted = !few && (by_seq || a.denom == 0.0);
     a.count = counted ? count : nullptr;
+    a.out[0] = x->loss;
+    a.out[1] = x->kl;
+    a.out[2] = x->clipped;
+    a.sync = few ? reinterpret_cast<uint32_t*>(ws + s.sync) : nullptr;
     a.part = reinterpret_cast<float*>(ws + s.part);
     if (counted) launch("loss count", k_loss_count, by_seq ? q.n : 1, 1024, 0, stream, r, q, (int)by_seq, count);
     loss_rows(rows->dtype, r, a, stream);
-    launch("loss total", k_loss_total, 3, 1024, 0, stream, a.part, r, 1.0, nullptr, x->loss, x->kl, x->clipped);
+    if (!few)
+      launch("loss total", k_loss_total, 3, 1024, 0, stream, a.part, r, 1.0, nullptr, x->loss, x->kl, x->clipped);
   });
 }
 
@@ -425,8 +393,8 @@ glr_status glr_distill_loss(const glr_loss_rows* rows, const glr_distill_args* x
     const Scratch s = scratch_of(GLR_LOSS_DISTILL, r.rows, 0, r.dz.p != nullptr);
     char* ws = check_ws(s, d_ws, ws_bytes);
     int* count = reinterpret_cast<int*>(ws + s.count);
-    const bool all = x->denominator == 0.0 && !r.y.p;        // every row is trained on
-    const bool counted = x->denominator == 0.0 && r.y.p;
+    const bool few = r.rows > 0 && r.rows <= kSelfCount;
+    const bool counted = !few && x->denominator == 0.0 && r.y.p;
     Teach q = {};
     q.ids = arr(x->ids);
     q.t = arr(x->teacher);
@@ -435,12 +403,16 @@ glr_status glr_distill_loss(const glr_loss_rows* rows, const glr_distill_args* x
     q.id64 = x->id_type == GLR_I64;
     q.ttype = x->teacher_type;
     q.hard = x->hard_weight;
-    q.denom = all ? (double)r.rows : x->denominator;
-    q.count = counted && r.rows > kSelfCount ? count : nullptr;
+    q.denom = x->denominator;
+    if (q.denom == 0.0 && !r.y.p) q.denom = r.rows ? (double)r.rows : 1.0;      // every row is trained on
+    q.count = counted ? count : nullptr;
     q.losses = x->losses;
-    if (q.count) launch("loss count", k_loss_count, 1, 1024, 0, stream, r, Seqs{}, 0, count);
+    q.loss = x->loss;
+    q.sync = few ? reinterpret_cast<uint32_t*>(ws + s.sync) : nullptr;
+    if (counted) launch("loss count", k_loss_count, 1, 1024, 0, stream, r, Seqs{}, 0, count);
     distill_rows(rows->dtype, r, q, stream);
-    launch("loss total", k_loss_total, 1, 1024, 0, stream, x->losses, r, q.denom, q.count, x->loss, nullptr, nullptr);
+    if (!few)
+      launch("loss total", k_loss_total, 1, 1024, 0, stream, x->losses, r, q.denom, q.count, x->loss, nullptr, nullptr);
   });
 }
 

@@ -1,0 +1,349 @@
+// Python binding of include/greedylore_losses.h: checks of the tensors,
+// results from torch's allocator, the call.  In C++ because a small loss is a
+// launch or two, and the same steps in Python took several times as long.
+//
+// Each function returns a tuple of results, or the glr_status of a refused
+// call as an int (its text is glr_last_error).
+#include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/utils/object_ptr.h>
+
+#include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
+
+#include <cstdarg>
+#include <map>
+#include <utility>
+#include <vector>
+
+#include "../../include/greedylore_losses.h"
+
+namespace {
+
+using at::Tensor;
+
+struct Status {
+  glr_status s;
+};
+void check(glr_status s) {
+  if (s != GLR_OK) throw Status{s};
+}
+
+// ---------------------------------------------------------------------------
+// arguments
+// ---------------------------------------------------------------------------
+[[noreturn]] void fail(PyObject* type, const char* format, ...) {
+  va_list ap;
+  va_start(ap, format);
+  PyErr_FormatV(type, format, ap);
+  va_end(ap);
+  throw python_error();
+}
+const Tensor& tensor(PyObject* o, const char* name) {
+  if (!THPVariable_Check(o)) fail(PyExc_TypeError, "%s must be a tensor, not %s", name, Py_TYPE(o)->tp_name);
+  return THPVariable_Unpack(o);
+}
+bool given(PyObject* o) { return o != Py_None; }
+double number(PyObject* o) {
+  const double x = PyFloat_AsDouble(o);
+  if (x == -1.0 && PyErr_Occurred()) throw python_error();
+  return x;
+}
+int64_t integer(PyObject* o) {
+  const int64_t x = PyLong_AsLongLong(o);
+  if (x == -1 && PyErr_Occurred()) throw python_error();
+  return x;
+}
+std::string text(at::IntArrayRef v) {
+  std::string s = "(";
+  for (size_t i = 0; i < v.size(); ++i) s += (i ? ", " : "") + std::to_string(v[i]);
+  return s + (v.size() == 1 ? ",)" : ")");
+}
+
+int float_type(at::ScalarType t) {
+  return t == at::kFloat ? GLR_F32 : t == at::kBFloat16 ? GLR_BF16 : t == at::kHalf ? GLR_F16 : -1;
+}
+int int_type(at::ScalarType t) { return t == at::kInt ? GLR_I32 : t == at::kLong ? GLR_I64 : -1; }
+
+// The rows of a call and what every argument is held against.
+struct Call {
+  glr_loss_rows r = {};
+  std::vector<int64_t> shape;      // of the rows
+  c10::Device device = c10::kCPU;
+  Tensor logits, dlogits;
+
+  int64_t rows() const { return r.batch * r.steps; }
+  Tensor empty(at::IntArrayRef s) const { return at::empty(s, at::TensorOptions().dtype(at::kFloat).device(device)); }
+
+  void same(const Tensor& x, const char* name, at::IntArrayRef want) const {
+    if (x.sizes() != want)
+      fail(PyExc_ValueError, "%s must have shape %s, not %s", name, text(want).c_str(), text(x.sizes()).c_str());
+    if (x.device() != device)
+      fail(PyExc_ValueError, "%s must live on %s, not %s", name, device.str().c_str(), x.device().str().c_str());
+  }
+  glr_row_array strided(const Tensor& x) const {
+    const auto st = x.strides();
+    return shape.size() == 2 ? glr_row_array{x.data_ptr(), st[0], st[1]} : glr_row_array{x.data_ptr(), 0, st[0]};
+  }
+  // an fp32 array over the rows
+  glr_row_array array(PyObject* o, const char* name) const {
+    const Tensor& x = tensor(o, name);
+    if (x.scalar_type() != at::kFloat)
+      fail(PyExc_TypeError, "%s must be torch.float32, not %s", name, c10::toString(x.scalar_type()));
+    same(x, name, shape);
+    return strided(x);
+  }
+  // one with a contiguous list in each row
+  glr_row_array lists(const Tensor& x, const char* name, int64_t n) const {
+    std::vector<int64_t> want(shape);
+    want.push_back(n);
+    same(x, name, want);
+    if (x.stride(-1) != 1 && n > 1) fail(PyExc_ValueError, "a row of %s must be contiguous", name);
+    return strided(x);
+  }
+
+  Call(PyObject* z, PyObject* y, PyObject* ignore, PyObject* temperature, bool grad, PyObject* scale, PyObject* out) {
+    logits = tensor(z, "logits");
+    r.dtype = float_type(logits.scalar_type());
+    if (r.dtype < 0)
+      fail(PyExc_TypeError, "logits must be float32, bfloat16 or float16, not %s", c10::toString(logits.scalar_type()));
+    const auto full = logits.sizes();
+    if (full.size() != 2 && full.size() != 3)
+      fail(PyExc_ValueError, "logits must be (rows, vocab) or (batch, steps, vocab), not %s", text(full).c_str());
+    if (!logits.is_cuda()) fail(PyExc_ValueError, "the losses run on the GPU only (logits on the CPU)");
+    shape.assign(full.begin(), full.end() - 1);
+    device = logits.device();
+    r.batch = shape.size() == 2 ? shape[0] : 1;
+    r.steps = shape.back();
+    r.vocab = full.back();
+    r.logits = lists(logits, "logits", r.vocab);
+    if (given(y)) {
+      const Tensor& t = tensor(y, "targets");
+      r.target_type = int_type(t.scalar_type());
+      if (r.target_type < 0)
+        fail(PyExc_TypeError, "targets must be int64 or int32, not %s", c10::toString(t.scalar_type()));
+      same(t, "targets", shape);
+      r.targets = strided(t);
+    }
+    if (!grad && given(out))
+      fail(PyExc_ValueError, "out is the gradient's: it needs grad=True (weights=... of token_logprobs)");
+    r.ignore_index = integer(ignore);
+    r.temperature = number(temperature);
+    r.grad_scale = number(scale);
+    if (!grad) return;
+    if (given(out)) {
+      dlogits = tensor(out, "out");
+      if (dlogits.scalar_type() != logits.scalar_type())
+        fail(PyExc_TypeError, "out must be %s, not %s", c10::toString(logits.scalar_type()),
+                               c10::toString(dlogits.scalar_type()));
+      r.dlogits = lists(dlogits, "out", r.vocab);
+      if (r.dlogits.data == r.logits.data && dlogits.strides() != logits.strides())
+        fail(PyExc_ValueError, "out that replaces the logits must have their strides");
+    } else {
+      dlogits = at::empty(full, logits.options().memory_format(at::MemoryFormat::Contiguous));
+      r.dlogits = strided(dlogits);
+    }
+  }
+
+  glr_loss_seqs seqs(PyObject* o) const {
+    if (!given(o)) {
+      if (shape.size() != 2) fail(PyExc_ValueError, "packed rows (2-D logits) need cu_seqlens");
+      return {shape[0], nullptr, 0};
+    }
+    const Tensor& cu = tensor(o, "cu_seqlens");
+    if (cu.dim() != 1 || cu.numel() < 2)
+      fail(PyExc_ValueError, "cu_seqlens must be one-dimensional with at least two offsets");
+    if (shape.size() != 1) fail(PyExc_ValueError, "cu_seqlens goes with packed rows (2-D logits)");
+    const int type = int_type(cu.scalar_type());
+    if (type < 0) fail(PyExc_TypeError, "cu_seqlens must be int64 or int32, not %s", c10::toString(cu.scalar_type()));
+    same(cu, "cu_seqlens", cu.sizes());
+    if (!cu.is_contiguous()) fail(PyExc_ValueError, "cu_seqlens must be contiguous");
+    return {cu.numel() - 1, cu.data_ptr(), type};
+  }
+};
+
+// Scratch.  One piece a stream, kept and grown: the calls of a stream follow
+// one another and leave its first words zero.  A call that is captured into a
+// graph gets its own, from the graph's memory, cleared in the graph.
+Tensor scratch(const Call& c, int op, int64_t seqs, void* stream, bool capturing, size_t* bytes) {
+  check(glr_loss_workspace_bytes(&c.r, op, seqs, bytes));
+  const auto make = [&](size_t n) {
+    Tensor t = at::empty({(int64_t)n}, at::TensorOptions().dtype(at::kByte).device(c.device));
+    t.narrow(0, 0, 16).zero_();
+    return t;
+  };
+  if (capturing) return make(*bytes);
+  static auto* kept = new std::map<std::pair<int, void*>, Tensor>();
+  Tensor& t = (*kept)[{c.device.index(), stream}];
+  if (!t.defined() || (size_t)t.numel() < *bytes) {
+    size_t n = 1 << 16;
+    while (n < *bytes) n *= 2;
+    t = Tensor();
+    t = make(n);
+  }
+  return t;
+}
+
+PyObject* wrap(const Tensor& t) {
+  if (t.defined()) return THPVariable_Wrap(t);
+  Py_RETURN_NONE;
+}
+template <class... T>
+PyObject* pack(const T&... t) {
+  PyObject* out = PyTuple_New(sizeof...(T));
+  if (!out) throw python_error();
+  Py_ssize_t i = 0;
+  (PyTuple_SET_ITEM(out, i++, wrap(t)), ...);
+  return out;
+}
+
+template <class F>
+PyObject* entry(Py_ssize_t n, Py_ssize_t want, F&& body) {
+  HANDLE_TH_ERRORS
+  if (n != want) fail(PyExc_TypeError, "%d arguments, %d wanted", (int)n, (int)want);
+  try {
+    return body();
+  } catch (const Status& s) {
+    return PyLong_FromLong(s.s);
+  }
+  END_HANDLE_TH_ERRORS
+}
+void* stream_of(PyObject* o) { return PyLong_AsVoidPtr(o); }
+
+// (stream, logits, targets, ignore_index, temperature, grad_scale, out, weights, want stats) -> logps, stats, dlogits
+PyObject* logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 9, [&] {
+    const bool grad = given(a[7]);
+    Call c(a[1], a[2], a[3], a[4], grad, a[5], a[6]);
+    glr_row_array w = {};
+    if (grad) w = c.array(a[7], "weights");
+    const c10::DeviceGuard guard(c.device);
+    const Tensor logps = c.empty(c.shape);
+    Tensor stats;
+    if (a[8] == Py_True) stats = c.empty({c.rows(), 2});
+    check(glr_token_logprobs(&c.r, grad ? &w : nullptr, logps.data_ptr<float>(),
+                             stats.defined() ? stats.data_ptr<float>() : nullptr, nullptr, 0, stream_of(a[0])));
+    return pack(logps, stats, c.dlogits);
+  });
+}
+
+// (stream, logits, targets, ignore_index, temperature, stats, grad_logps) -> dlogits
+PyObject* logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 7, [&] {
+    PyObject* one = PyFloat_FromDouble(1.0);
+    const THPObjectPtr hold(one);
+    Call c(a[1], a[2], a[3], a[4], true, one, Py_None);
+    const glr_row_array g = c.array(a[6], "the upstream gradient");
+    const c10::DeviceGuard guard(c.device);
+    check(glr_token_logprobs_backward(&c.r, tensor(a[5], "stats").data_ptr<float>(), &g, stream_of(a[0])));
+    return pack(c.dlogits);
+  });
+}
+
+// (stream, capturing, logits, targets, ignore_index, grad, grad_scale, out, ref_logps, beta, kind, label_smoothing,
+//  average, cu_seqlens, temperature) -> loss, logps, rewards, dlogits
+PyObject* preference(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 15, [&] {
+    Call c(a[2], a[3], a[4], a[14], a[5] == Py_True, a[6], a[7]);
+    glr_pref_args x = {};
+    x.seqs = c.seqs(a[13]);
+    const Tensor& ref = tensor(a[8], "ref_logps");
+    if (ref.scalar_type() != at::kFloat)
+      fail(PyExc_TypeError, "ref_logps must be torch.float32, not %s", c10::toString(ref.scalar_type()));
+    c.same(ref, "ref_logps", {x.seqs.seqs});
+    if (!ref.is_contiguous()) fail(PyExc_ValueError, "ref_logps must be contiguous");
+    const c10::DeviceGuard guard(c.device);
+    const Tensor loss = c.empty({}), logps = c.empty({x.seqs.seqs}), rewards = c.empty({x.seqs.seqs});
+    x.kind = (int32_t)integer(a[10]);
+    x.average = a[12] == Py_True;
+    x.beta = number(a[9]);
+    x.label_smoothing = number(a[11]);
+    x.ref_logps = ref.data_ptr<float>();
+    x.loss = loss.data_ptr<float>();
+    x.logps = logps.data_ptr<float>();
+    x.rewards = rewards.data_ptr<float>();
+    size_t bytes = 0;
+    const Tensor ws = scratch(c, GLR_LOSS_PREFERENCE, x.seqs.seqs, stream_of(a[0]), a[1] == Py_True, &bytes);
+    check(glr_preference_loss(&c.r, &x, ws.data_ptr(), bytes, stream_of(a[0])));
+    return pack(loss, logps, rewards, c.dlogits);
+  });
+}
+
+// (stream, capturing, logits, targets, ignore_index, temperature, grad, grad_scale, out, old_logps, advantages,
+//  ref_logps, clip_low, clip_high, kl_coef, reduction, denominator, cu_seqlens) -> loss, logps, kl, clipped, dlogits
+PyObject* policy(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 18, [&] {
+    Call c(a[2], a[3], a[4], a[5], a[6] == Py_True, a[7], a[8]);
+    glr_policy_args x = {};
+    x.reduction = (int32_t)integer(a[15]);
+    if (given(a[17]) || x.reduction == GLR_REDUCE_SEQUENCE) x.seqs = c.seqs(a[17]);
+    x.old_logps = c.array(a[9], "old_logps");
+    x.advantages = c.array(a[10], "advantages");
+    if (given(a[11])) x.ref_logps = c.array(a[11], "ref_logps");
+    x.clip_low = number(a[12]);
+    x.clip_high = number(a[13]);
+    x.kl_coef = number(a[14]);
+    x.denominator = number(a[16]);
+    const c10::DeviceGuard guard(c.device);
+    const Tensor loss = c.empty({}), kl = c.empty({}), clipped = c.empty({}), logps = c.empty(c.shape);
+    x.loss = loss.data_ptr<float>();
+    x.kl = kl.data_ptr<float>();
+    x.clipped = clipped.data_ptr<float>();
+    x.logps = logps.data_ptr<float>();
+    size_t bytes = 0;
+    const Tensor ws = scratch(c, GLR_LOSS_POLICY, x.seqs.seqs, stream_of(a[0]), a[1] == Py_True, &bytes);
+    check(glr_policy_loss(&c.r, &x, ws.data_ptr(), bytes, stream_of(a[0])));
+    return pack(loss, logps, kl, clipped, c.dlogits);
+  });
+}
+
+// (stream, capturing, logits, targets, ignore_index, temperature, grad, grad_scale, out, teacher_ids, teacher_logits,
+//  teacher_lse, hard_weight, denominator) -> loss, losses, dlogits
+PyObject* distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 14, [&] {
+    Call c(a[2], a[3], a[4], a[5], a[6] == Py_True, a[7], a[8]);
+    const Tensor &ids = tensor(a[9], "teacher_ids"), &t = tensor(a[10], "teacher_logits");
+    if (ids.dim() != (int64_t)c.shape.size() + 1) fail(PyExc_ValueError, "teacher_ids must have the logits' dimensions");
+    glr_distill_args x = {};
+    x.id_type = int_type(ids.scalar_type());
+    x.teacher_type = float_type(t.scalar_type());
+    if (x.id_type < 0) fail(PyExc_TypeError, "teacher_ids must be int64 or int32, not %s", c10::toString(ids.scalar_type()));
+    if (x.teacher_type < 0)
+      fail(PyExc_TypeError, "teacher_logits must be float32, bfloat16 or float16, not %s", c10::toString(t.scalar_type()));
+    const int64_t top = ids.size(-1);
+    x.top = (int32_t)std::min<int64_t>(top, INT32_MAX);
+    x.ids = c.lists(ids, "teacher_ids", top);
+    x.teacher = c.lists(t, "teacher_logits", top);
+    if (given(a[11])) x.teacher_lse = c.array(a[11], "teacher_lse");
+    x.hard_weight = number(a[12]);
+    x.denominator = number(a[13]);
+    const c10::DeviceGuard guard(c.device);
+    const Tensor loss = c.empty({}), losses = c.empty(c.shape);
+    x.loss = loss.data_ptr<float>();
+    x.losses = losses.data_ptr<float>();
+    size_t bytes = 0;
+    const Tensor ws = scratch(c, GLR_LOSS_DISTILL, 0, stream_of(a[0]), a[1] == Py_True, &bytes);
+    check(glr_distill_loss(&c.r, &x, ws.data_ptr(), bytes, stream_of(a[0])));
+    return pack(loss, losses, c.dlogits);
+  });
+}
+
+// (stream, gradient, upstream gradient): the first times the second, in place
+PyObject* rescale(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 3, [&]() -> PyObject* {
+    const Tensor &d = tensor(a[1], "the gradient"), &scale = tensor(a[2], "the upstream gradient");
+    const c10::DeviceGuard guard(d.device());
+    check(glr_loss_rescale(d.data_ptr(), d.numel(), float_type(d.scalar_type()), scale.data_ptr<float>(), stream_of(a[0])));
+    Py_RETURN_NONE;
+  });
+}
+
+#define FAST(name) \
+  { #name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr }
+PyMethodDef methods[] = {FAST(logprobs), FAST(logprobs_backward), FAST(preference), FAST(policy), FAST(distill),
+                         FAST(rescale), {nullptr, nullptr, 0, nullptr}};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_losses", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__losses() { return PyModule_Create(&module); }

@@ -19,19 +19,74 @@ HEADER = os.path.join(ROOT, "include", "greedylore_losses.h")
 PTR = 0x10000       # aligned, never followed
 
 
+# ----------------------------------------------------------------------------
+# the C ABI, as a caller with structs of its own sees it
+# ----------------------------------------------------------------------------
+I32, I64, F64, VP, SZ, P = ctypes.c_int32, ctypes.c_int64, ctypes.c_double, ctypes.c_void_p, ctypes.c_size_t, ctypes.POINTER
+
+
+class RowArray(ctypes.Structure):
+    _fields_ = [("data", VP), ("stride_b", I64), ("stride_s", I64)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("batch", I64), ("steps", I64), ("vocab", I64), ("logits", RowArray), ("dlogits", RowArray),
+                ("dtype", I32), ("target_type", I32), ("targets", RowArray), ("ignore_index", I64), ("temperature", F64),
+                ("grad_scale", F64)]
+
+
+class Seqs(ctypes.Structure):
+    _fields_ = [("seqs", I64), ("cu_seqlens", VP), ("cu_type", I32)]
+
+
+class PrefArgs(ctypes.Structure):
+    _fields_ = [("seqs", Seqs), ("kind", I32), ("average", I32), ("beta", F64), ("label_smoothing", F64),
+                ("ref_logps", VP), ("loss", VP), ("logps", VP), ("rewards", VP)]
+
+
+class PolicyArgs(ctypes.Structure):
+    _fields_ = [("seqs", Seqs), ("reduction", I32), ("clip_low", F64), ("clip_high", F64), ("kl_coef", F64),
+                ("denominator", F64), ("old_logps", RowArray), ("advantages", RowArray), ("ref_logps", RowArray),
+                ("loss", VP), ("kl", VP), ("clipped", VP), ("logps", VP)]
+
+
+class DistillArgs(ctypes.Structure):
+    _fields_ = [("top", I32), ("id_type", I32), ("teacher_type", I32), ("ids", RowArray), ("teacher", RowArray),
+                ("teacher_lse", RowArray), ("hard_weight", F64), ("denominator", F64), ("loss", VP), ("losses", VP)]
+
+
+SIGNATURES = {
+    "glr_loss_workspace_bytes": [P(Rows), I32, I64, P(SZ)],
+    "glr_token_logprobs": [P(Rows), P(RowArray), VP, VP, VP, SZ, VP],
+    "glr_token_logprobs_backward": [P(Rows), VP, P(RowArray), VP],
+    "glr_preference_loss": [P(Rows), P(PrefArgs), VP, SZ, VP],
+    "glr_policy_loss": [P(Rows), P(PolicyArgs), VP, SZ, VP],
+    "glr_distill_loss": [P(Rows), P(DistillArgs), VP, SZ, VP],
+    "glr_loss_rescale": [VP, I64, I32, VP, VP],
+}
+
+
+def _lib():
+    lib = glr.load()
+    for name, args in SIGNATURES.items():
+        fn = getattr(lib, name)
+        fn.restype, fn.argtypes = I32, args
+    return lib
+
+
 def test_library_exports_every_declared_symbol():
     text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
     names = set(re.findall(r"\b(glr_[a-z_0-9]+)\s*\(", text))
-    assert names == set(losses.LOSS_EXPORTED)
+    assert names == set(SIGNATURES)
     lib = glr.load()
     for name in names:
         assert hasattr(lib, name), name
 
 
 def test_struct_layouts_match_the_header(tmp_path):
-    pairs = [("glr_row_array", losses.RowArray), ("glr_loss_rows", losses.Rows), ("glr_loss_seqs", losses.Seqs),
-             ("glr_pref_args", losses.PrefArgs), ("glr_policy_args", losses.PolicyArgs),
-             ("glr_distill_args", losses.DistillArgs)]
+    pairs = [("glr_row_array", RowArray), ("glr_loss_rows", Rows), ("glr_loss_seqs", Seqs),
+             ("glr_pref_args", PrefArgs), ("glr_policy_args", PolicyArgs),
+             ("glr_distill_args", DistillArgs)]
     lines = []
     for c, py in pairs:
         lines.append(f'printf("{c} %zu\\n", sizeof({c}));')
@@ -51,14 +106,14 @@ def _rows(**kw):
     a = dict(batch=2, steps=3, vocab=50, logits=(PTR, 150, 50), dlogits=(PTR, 150, 50), dtype=0, target_type=1,
              targets=(PTR, 3, 1), ignore_index=-100, temperature=1.0, grad_scale=1.0)
     a.update(kw)
-    return losses.Rows(*[a[f[0]] for f in losses.Rows._fields_])
+    return Rows(*[a[f[0]] for f in Rows._fields_])
 
 
 def _pref(**kw):
     a = dict(seqs=(2, None, 0), kind=0, average=0, beta=0.1, label_smoothing=0.0, ref_logps=PTR, loss=PTR, logps=PTR,
              rewards=PTR)
     a.update(kw)
-    return losses.PrefArgs(*[a[f[0]] for f in losses.PrefArgs._fields_])
+    return PrefArgs(*[a[f[0]] for f in PrefArgs._fields_])
 
 
 def _policy(**kw):
@@ -66,18 +121,18 @@ def _policy(**kw):
              old_logps=(PTR, 3, 1), advantages=(PTR, 3, 1), ref_logps=(None, 0, 0), loss=PTR, kl=PTR, clipped=PTR,
              logps=PTR)
     a.update(kw)
-    return losses.PolicyArgs(*[a[f[0]] for f in losses.PolicyArgs._fields_])
+    return PolicyArgs(*[a[f[0]] for f in PolicyArgs._fields_])
 
 
 def _distill(**kw):
     a = dict(top=4, id_type=0, teacher_type=0, ids=(PTR, 12, 4), teacher=(PTR, 12, 4), teacher_lse=(None, 0, 0),
              hard_weight=0.0, denominator=0.0, loss=PTR, losses=PTR)
     a.update(kw)
-    return losses.DistillArgs(*[a[f[0]] for f in losses.DistillArgs._fields_])
+    return DistillArgs(*[a[f[0]] for f in DistillArgs._fields_])
 
 
 WS = (PTR, 1 << 20)
-W = losses.RowArray(PTR, 3, 1)
+W = RowArray(PTR, 3, 1)
 NAN, INF = float("nan"), float("inf")
 
 
@@ -89,7 +144,7 @@ NAN, INF = float("nan"), float("inf")
     (dict(dlogits=(PTR + 1, 150, 50)), 1), (dict(targets=(None, 0, 0)), 1), (dict(targets=(PTR + 4, 3, 1)), 1),
 ])
 def test_bad_rows_are_refused_by_every_entry(kw, code):
-    lib, r = losses._lib(), _rows(**kw)
+    lib, r = _lib(), _rows(**kw)
     assert lib.glr_token_logprobs(r, W, PTR, None, None, 0, None) == code
     assert lib.glr_last_error(None).decode()
     assert lib.glr_token_logprobs_backward(r, PTR, W, None) == code
@@ -100,7 +155,7 @@ def test_bad_rows_are_refused_by_every_entry(kw, code):
 
 
 def test_null_structs_and_outputs_are_refused():
-    lib, r, n = losses._lib(), _rows(), ctypes.c_size_t()
+    lib, r, n = _lib(), _rows(), ctypes.c_size_t()
     assert lib.glr_loss_workspace_bytes(None, 0, 0, n) == 1
     assert lib.glr_loss_workspace_bytes(r, 0, 0, None) == 1
     assert lib.glr_loss_workspace_bytes(r, 9, 0, n) == 1
@@ -126,7 +181,7 @@ def test_null_structs_and_outputs_are_refused():
     (dict(label_smoothing=1.0), 1), (dict(label_smoothing=-0.1), 1), (dict(label_smoothing=0.1, kind=1), 1),
     (dict(ref_logps=None), 1), (dict(loss=None), 1), (dict(logps=None), 1), (dict(rewards=None), 1)])
 def test_bad_preference_arguments_are_refused(kw, code):
-    assert losses._lib().glr_preference_loss(_rows(), _pref(**kw), *WS, None) == code
+    assert _lib().glr_preference_loss(_rows(), _pref(**kw), *WS, None) == code
 
 
 @pytest.mark.parametrize("kw,code", [
@@ -137,7 +192,7 @@ def test_bad_preference_arguments_are_refused(kw, code):
     (dict(advantages=(None, 0, 0)), 1), (dict(ref_logps=(PTR + 1, 3, 1)), 1), (dict(loss=None), 1), (dict(kl=None), 1),
     (dict(clipped=None), 1), (dict(logps=None), 1)])
 def test_bad_policy_arguments_are_refused(kw, code):
-    assert losses._lib().glr_policy_loss(_rows(), _policy(**kw), *WS, None) == code
+    assert _lib().glr_policy_loss(_rows(), _policy(**kw), *WS, None) == code
 
 
 @pytest.mark.parametrize("kw,code", [
@@ -146,17 +201,17 @@ def test_bad_policy_arguments_are_refused(kw, code):
     (dict(hard_weight=-0.1), 1), (dict(hard_weight=1.1), 1), (dict(hard_weight=NAN), 1), (dict(denominator=-1.0), 1),
     (dict(loss=None), 1), (dict(losses=None), 1)])
 def test_bad_distillation_arguments_are_refused(kw, code):
-    assert losses._lib().glr_distill_loss(_rows(), _distill(**kw), *WS, None) == code
+    assert _lib().glr_distill_loss(_rows(), _distill(**kw), *WS, None) == code
 
 
 def test_distillation_limits():
-    lib = losses._lib()
+    lib = _lib()
     assert lib.glr_distill_loss(_rows(vocab=(1 << 19) + 1), _distill(), *WS, None) == 2
     assert lib.glr_distill_loss(_rows(targets=(None, 0, 0)), _distill(hard_weight=0.5), *WS, None) == 1
 
 
 def test_workspaces_are_checked():
-    lib, r = losses._lib(), _rows()
+    lib, r = _lib(), _rows()
     for op, fn, args, seqs in ((1, lib.glr_preference_loss, _pref(), 2), (2, lib.glr_policy_loss, _policy(), 0),
                                (3, lib.glr_distill_loss, _distill(), 0)):
         n = ctypes.c_size_t()
