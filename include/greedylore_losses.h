@@ -44,11 +44,12 @@
  * buffer; the calls only enqueue, on `stream`, and may be captured into a HIP
  * graph; they keep nothing between calls.  d_ws is scratch of at least
  * glr_loss_workspace_bytes bytes, 16-byte aligned, in use until the call's
- * work has run; its first 16 bytes must be zero then, and the call leaves
- * them zero (waves that finish count themselves there): scratch that was
- * cleared once serves any number of calls on one stream, of any of the losses,
- * and calls that may run at the same time need scratch of their own.  Argument errors are found before anything is enqueued; the
- * text is glr_last_error(NULL).
+ * work has run; its first GLR_LOSS_SYNC_BYTES must be zero then, and the call
+ * leaves them zero (waves that finish count themselves there): scratch that
+ * was cleared once serves any number of calls on one stream, of any of the
+ * losses; calls that may run at the same time need scratch of their own.
+ * Argument errors are found before anything is enqueued; the text is
+ * glr_last_error(NULL).
  */
 #ifndef GREEDYLORE_LOSSES_H
 #define GREEDYLORE_LOSSES_H
@@ -58,6 +59,8 @@
 #ifdef __cplusplus
 extern "C" {
 #endif
+
+#define GLR_LOSS_SYNC_BYTES 64
 
 typedef enum { GLR_F32 = 0, GLR_BF16 = 1, GLR_F16 = 2 } glr_dtype;
 typedef enum { GLR_I32 = 0, GLR_I64 = 1 } glr_itype;

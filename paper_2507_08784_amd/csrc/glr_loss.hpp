@@ -22,11 +22,12 @@ typedef _Float16 f16_t;
 
 constexpr int kLT = 256;                        // threads of the small kernels
 constexpr int kMaxTop = 1024;
-// A call of up to kSelfCount rows is one launch (two with a preference's
-// gradient): every row's wave counts the rows trained on itself (16 loads a
-// lane, beside the row's), and the last wave to arrive makes the totals.
-constexpr uint32_t kSelfCount = 1024;
-constexpr int32_t kSelfSeqs = 64;               // sequences of such a preference loss
+// A policy or distillation call of up to kSelfCount rows is one launch: every
+// row's wave counts the rows trained on itself (4 loads a lane, beside the
+// row's), and the last wave to arrive makes the totals.  A call on 264 rows
+// took 13 us so and 19 with launches of their own for the count and the
+// totals, one on 918 rows 25 and 19 (the arrivals come one after the other).
+constexpr uint32_t kSelfCount = 256;
 constexpr int64_t kMaxLossVocab = (int64_t)1 << 28;
 constexpr int64_t kMaxDistillVocab = (int64_t)1 << 19;   // the list's bitmap stays within 64 KB of LDS
 constexpr double kRestFloor = 1.0 / (1 << 20);
@@ -109,21 +110,6 @@ __device__ __forceinline__ bool row_target(const Rows& r, const RowPos& p, int& 
 
 enum { OP_LOGP, OP_POLICY, OP_COEF };
 
-// The pairs of a preference loss.
-struct Pairs {
-  Seqs seqs;
-  int kind, average;
-  double beta, smooth;
-  const float* ref;
-  float* loss;
-  float* logps;
-  float* rewards;
-  const float* lp;     // of the rows
-  float* coef;         // d loss / d lp of a sequence's rows
-  float* part;         // a pair's loss
-  uint32_t* sync;
-};
-
 struct Terms {
   int32_t op;
   int32_t again;             // the logits are read again right after
@@ -141,10 +127,7 @@ struct Terms {
   const int* count;
   float* part;               // 3 x rows: w term, w kl, w clipped
   float* out[3];             // their sums
-  // The last wave to arrive makes the call's totals (NULL: a launch of their
-  // own does): of the policy's parts, or the pairs of a preference loss.
-  uint32_t* sync;
-  Pairs pairs;
+  uint32_t* sync;            // the last wave to arrive makes the sums (NULL: a launch of their own does)
 };
 
 // ---------------------------------------------------------------------------
@@ -278,39 +261,6 @@ __device__ __forceinline__ double total_of(const float* part, uint32_t n) {
   double x = 0.0;
   for (uint32_t i = threadIdx.x & 63; i < n; i += 64) x += get_shared(part + i);
   return wave_sum(x);
-}
-
-// a pair's loss and what its sequences' rows get, from the sums of their log-probabilities
-__device__ __forceinline__ void pair_terms(const Pairs& q, int i, double L0, int n0, double L1, int n1) {
-  const int half = q.seqs.n >> 1, j = i + half;
-  n0 = max(n0, 1);
-  n1 = max(n1, 1);
-  L0 /= n0;
-  L1 /= n1;
-  const double rc = L0 - (double)q.ref[i], rr = L1 - (double)q.ref[j];
-  const double delta = rc - rr, h = q.beta * delta;
-  double loss, slope;
-  if (q.kind == GLR_PREF_SIGMOID) {
-    const double soft = log1p(exp(-fabs(h)));
-    const double neg = soft + (h < 0.0 ? -h : 0.0), pos = soft + (h > 0.0 ? h : 0.0);   // -log sigma(h), -log sigma(-h)
-    loss = (1.0 - q.smooth) * neg + q.smooth * pos;
-    slope = q.beta * (q.smooth - 1.0 / (1.0 + exp(h)));
-    if (h != h) loss = h;
-  } else if (q.kind == GLR_PREF_HINGE) {
-    loss = h < 1.0 ? 1.0 - h : h == h ? 0.0 : h;
-    slope = h < 1.0 ? -q.beta : h == h ? 0.0 : h;
-  } else {
-    const double off = delta - 0.5 / q.beta;
-    loss = off * off;
-    slope = 2.0 * off;
-  }
-  q.logps[i] = (float)L0;
-  q.logps[j] = (float)L1;
-  q.rewards[i] = (float)(q.beta * rc);
-  q.rewards[j] = (float)(q.beta * rr);
-  q.coef[i] = (float)(slope / half / n0);
-  q.coef[j] = (float)(-slope / half / n1);
-  put_shared(q.part + i, (float)loss);
 }
 
 // ---------------------------------------------------------------------------

@@ -43,7 +43,7 @@ __device__ __forceinline__ int self_count(const Rows& r, const Terms& a, int seq
 __device__ __forceinline__ double row_terms(const Rows& r, const Terms& a, const RowPos& p, const RowIn& x, float m,
                                             float s) {
   const double lp = ((double)x.zy - (double)m) * r.inv_t - log((double)s);
-  put_shared(a.logps + p.t, (float)lp);
+  a.logps[p.t] = (float)lp;
   if (a.op == OP_LOGP) {
     if (a.stats) {
       a.stats[2 * (int64_t)p.t] = m;
@@ -69,7 +69,7 @@ __device__ __forceinline__ double row_terms(const Rows& r, const Terms& a, const
 }
 // what a masked row leaves
 __device__ __forceinline__ void row_masked(const Rows& r, const Terms& a, const RowPos& p) {
-  put_shared(a.logps + p.t, 0.f);
+  a.logps[p.t] = 0.f;
   if (a.op == OP_LOGP) {
     if (a.stats) {
       a.stats[2 * (int64_t)p.t] = 0.f;
@@ -83,30 +83,10 @@ __device__ __forceinline__ void row_masked(const Rows& r, const Terms& a, const 
 // A wave has stored its rows' terms: the last of the call's makes the totals.
 __device__ __forceinline__ void row_done(const Rows& r, const Terms& a, uint32_t waves) {
   if (!a.sync || !last_to_arrive(a.sync, waves)) return;
-  const int lane = threadIdx.x & 63;
-  if (a.op == OP_POLICY) {
-    for (int k = 0; k < 3; ++k) {
-      const double x = total_of(a.part + k * (int64_t)r.rows, r.rows);
-      if (lane == 0) *a.out[k] = (float)x;
-    }
-    return;
+  for (int k = 0; k < 3; ++k) {
+    const double x = total_of(a.part + k * (int64_t)r.rows, r.rows);
+    if ((threadIdx.x & 63) == 0) *a.out[k] = (float)x;
   }
-  const Pairs& q = a.pairs;
-  const int half = q.seqs.n >> 1;
-  for (int i = 0; i < half; ++i) {
-    double L[2];
-    int n[2] = {1, 1};
-    for (int side = 0; side < 2; ++side) {
-      uint32_t lo, hi;
-      seq_span(r, q.seqs, i + side * (int64_t)half, lo, hi);
-      L[side] = total_of(q.lp + lo, hi > lo ? hi - lo : 0);      // (0 where masked)
-      if (q.average) n[side] = count_span(r, lo, hi);
-    }
-    if (lane == 0) pair_terms(q, i, L[0], n[0], L[1], n[1]);
-  }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // lane 0's parts
-  const double loss = total_of(q.part, half);
-  if (lane == 0) *q.loss = (float)(loss / half);
 }
 
 // whether a row is trained on; its target and its sequence

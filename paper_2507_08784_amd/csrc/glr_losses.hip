@@ -37,6 +37,54 @@ __global__ void __launch_bounds__(1024) k_loss_count(Rows r, Seqs q, int by_seq,
   if (threadIdx.x == 0) count[blockIdx.x] = n;
 }
 
+// The pairs of a preference loss.
+struct Pairs {
+  Seqs seqs;
+  int kind, average;
+  double beta, smooth;
+  const float* ref;
+  float* loss;
+  float* logps;
+  float* rewards;
+  const float* lp;     // of the rows
+  float* coef;         // d loss / d lp of a sequence's rows
+  float* part;         // a pair's loss
+  uint32_t* sync;
+};
+
+// a pair's loss and what its sequences' rows get, from the sums of their log-probabilities
+__device__ __forceinline__ float pair_terms(const Pairs& q, int i, double L0, int n0, double L1, int n1) {
+  const int half = q.seqs.n >> 1, j = i + half;
+  n0 = max(n0, 1);
+  n1 = max(n1, 1);
+  L0 /= n0;
+  L1 /= n1;
+  const double rc = L0 - (double)q.ref[i], rr = L1 - (double)q.ref[j];
+  const double delta = rc - rr, h = q.beta * delta;
+  double loss, slope;
+  if (q.kind == GLR_PREF_SIGMOID) {
+    const double soft = log1p(exp(-fabs(h)));
+    const double neg = soft + (h < 0.0 ? -h : 0.0), pos = soft + (h > 0.0 ? h : 0.0);   // -log sigma(h), -log sigma(-h)
+    loss = (1.0 - q.smooth) * neg + q.smooth * pos;
+    slope = q.beta * (q.smooth - 1.0 / (1.0 + exp(h)));
+    if (h != h) loss = h;
+  } else if (q.kind == GLR_PREF_HINGE) {
+    loss = h < 1.0 ? 1.0 - h : h == h ? 0.0 : h;
+    slope = h < 1.0 ? -q.beta : h == h ? 0.0 : h;
+  } else {
+    const double off = delta - 0.5 / q.beta;
+    loss = off * off;
+    slope = 2.0 * off;
+  }
+  q.logps[i] = (float)L0;
+  q.logps[j] = (float)L1;
+  q.rewards[i] = (float)(q.beta * rc);
+  q.rewards[j] = (float)(q.beta * rr);
+  q.coef[i] = (float)(slope / half / n0);
+  q.coef[j] = (float)(-slope / half / n1);
+  return (float)loss;
+}
+
 // A workgroup a pair; the last one adds the pairs' losses.
 __global__ void __launch_bounds__(1024) k_loss_pairs(Rows r, Pairs q) {
   __shared__ double shd[16];
@@ -58,7 +106,7 @@ __global__ void __launch_bounds__(1024) k_loss_pairs(Rows r, Pairs q) {
     n[side] = q.average ? block_sum<1024, int>(c, shi) : 1;
   }
   if (threadIdx.x >= 64) return;
-  if (threadIdx.x == 0) pair_terms(q, blockIdx.x, L[0], n[0], L[1], n[1]);
+  if (threadIdx.x == 0) put_shared(q.part + blockIdx.x, pair_terms(q, blockIdx.x, L[0], n[0], L[1], n[1]));
   if (last_to_arrive(q.sync, gridDim.x)) {
     const double loss = total_of(q.part, gridDim.x);
     if (threadIdx.x == 0) *q.loss = (float)(loss / half);
@@ -179,7 +227,7 @@ struct Scratch {
 };
 Scratch scratch_of(int op, int64_t rows, int64_t seqs, bool grad) {
   Scratch s;
-  if (op != GLR_LOSS_LOGPROBS) s.sync = s.take(16);
+  if (op != GLR_LOSS_LOGPROBS) s.sync = s.take(GLR_LOSS_SYNC_BYTES);
   if (op == GLR_LOSS_PREFERENCE) {
     s.lp = s.take(4 * rows);
     s.stats = s.take(grad ? 8 * rows : 0);
@@ -275,13 +323,12 @@ glr_status glr_preference_loss(const glr_loss_rows* rows, const glr_pref_args* x
     check_out(x->rewards, "rewards");
     const Scratch s = scratch_of(GLR_LOSS_PREFERENCE, r.rows, q.n, r.dz.p != nullptr);
     char* ws = check_ws(s, d_ws, ws_bytes);
-    uint32_t* sync = reinterpret_cast<uint32_t*>(ws + s.sync);
     Terms a = {};
     a.op = OP_LOGP;
     a.seqs = q;
     a.logps = reinterpret_cast<float*>(ws + s.lp);
     a.stats = r.dz.p ? reinterpret_cast<float*>(ws + s.stats) : nullptr;
-    Pairs& b = a.pairs;
+    Pairs b = {};
     b.seqs = q;
     b.kind = x->kind;
     b.average = x->average;
@@ -294,14 +341,12 @@ glr_status glr_preference_loss(const glr_loss_rows* rows, const glr_pref_args* x
     b.lp = a.logps;
     b.coef = reinterpret_cast<float*>(ws + s.coef);
     b.part = reinterpret_cast<float*>(ws + s.part);
-    b.sync = sync;
-    const bool few = r.rows > 0 && r.rows <= kSelfCount && q.n <= kSelfSeqs;
-    a.sync = few ? sync : nullptr;
+    b.sync = reinterpret_cast<uint32_t*>(ws + s.sync);
     a.again = r.dz.p != nullptr;
     Rows f = r;
     f.dz.p = nullptr;
     loss_rows(rows->dtype, f, a, stream);
-    if (!few) launch("loss pairs", k_loss_pairs, q.n / 2, 1024, 0, stream, r, b);
+    launch("loss pairs", k_loss_pairs, q.n / 2, 1024, 0, stream, r, b);
     if (r.dz.p) {
       a.op = OP_COEF;
       a.seq_coef = b.coef;

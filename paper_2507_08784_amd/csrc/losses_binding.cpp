@@ -169,7 +169,7 @@ Tensor scratch(const Call& c, int op, int64_t seqs, void* stream, bool capturing
   check(glr_loss_workspace_bytes(&c.r, op, seqs, bytes));
   const auto make = [&](size_t n) {
     Tensor t = at::empty({(int64_t)n}, at::TensorOptions().dtype(at::kByte).device(c.device));
-    t.narrow(0, 0, 16).zero_();
+    t.narrow(0, 0, GLR_LOSS_SYNC_BYTES).zero_();
     return t;
   };
   if (capturing) return make(*bytes);
