@@ -419,6 +419,68 @@ def test_policy_loss(L, dtype, V, layout, reduction, kl):
         close(s.loss, loss / 4, dloss, "loss over a given count")
 
 
+# calls of up to 256 rows make their totals themselves, from 8193 rows on short rows share a wave
+@pytest.mark.parametrize("reduction", ["token", "sequence"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,S,V", [(5, 51, 77), (1, 256, 300), (257, 1, 1100), (3, 2735, 90), (2, 4099, 333), (41, 200, 700),
+                                   (7, 1200, 1500), (3, 100, 5000)])
+def test_policy_loss_over_many_rows(L, B, S, V, dtype, reduction):
+    rows, kl = B * S, 0.1
+    z, y, gen = make(rows, V, dtype, rows + V, masked=0.4)
+    y.view(B, S)[B // 2] = IGNORE              # a sequence with nothing to train on
+    y[0] = 1
+    lp, p = ref_rows(z, y, 1.0)
+    d = 0.3 * torch.randn(rows, generator=gen).double()
+    for edge in (math.log1p(-0.2), math.log1p(0.2)):
+        d = torch.where((d - edge).abs() < 1e-3, d + 4e-3, d)
+    old, adv = (lp - d).float(), torch.randn(rows, generator=gen)
+    ref = (lp + 0.5 * torch.randn(rows, generator=gen)).float()
+    live = y != IGNORE
+    if reduction == "token":
+        w = torch.full((rows,), 1.0 / int(live.sum())).double()
+    else:
+        w = (1.0 / (B * live.view(B, S).sum(1, keepdim=True).clamp(min=1).double())).expand(B, S).reshape(-1)
+    loss, dloss, k, cut, coef, dcoef = ref_policy(lp, y, w, old.double(), adv.double(), ref.double(), 0.2, 0.2, kl)
+    r = L.policy_loss(z.cuda().view(B, S, V), *[x.cuda().view(B, S) for x in (y, old, adv)], ref_logps=ref.cuda().view(B, S),
+                      kl_coef=kl, reduction=reduction, grad=True)
+    close(r.loss, loss, dloss, "loss")
+    close(r.kl, k, dloss, "kl")
+    close(r.clipped, cut, 4 * U, "clipped")
+    close(r.logps, torch.where(live, lp, 0.0), lp_tol(lp), "logps")
+    close_grad(r.dlogits, ref_grad(p, y, coef, 1.0), p, y, coef, dcoef, 1.0, dtype, "dlogits")
+
+
+@pytest.mark.parametrize("rows", [255, 256, 257, 1500])
+def test_distillation_totals(L, rows):
+    V, K = 260, 9
+    z, y, gen = make(rows, V, torch.bfloat16, rows)
+    ids = torch.stack([torch.randperm(V, generator=gen)[:K] for _ in range(rows)])
+    t = torch.randn(rows, K, generator=gen)
+    r = L.distill_loss(z.cuda(), ids.cuda(), t.cuda(), targets=y.cuda(), hard_weight=0.2, temperature=1.5, grad=True)
+    n = int((y != IGNORE).sum())
+    per, grad, ptol, tol = ref_distill(z, ids, t, y, 1.5, None, 0.2, n)
+    close(r.losses, per, ptol, "losses")
+    close(r.loss, per.sum() / n, ptol.sum() / n, "loss")
+    off = (r.dlogits.double().cpu() - grad).abs()
+    assert bool((off <= tol + HALF_ULP[torch.bfloat16] * 1.001 * grad.abs() + TINY[torch.bfloat16]).all())
+
+
+def test_many_pairs(L):
+    n, V = 600, 64                              # 300 pairs of one to four rows
+    gen = torch.Generator().manual_seed(3)
+    ends = [0] + torch.randint(0, 5, (n,), generator=gen).cumsum(0).tolist()
+    rows = ends[-1]
+    z, y, gen = make(rows, V, torch.float32, 8, masked=0.2)
+    lp, p = ref_rows(z, y, 1.0)
+    ref = -6.0 * torch.rand(n, generator=gen)
+    spans = list(zip(ends[:-1], ends[1:]))
+    loss, dl, seq, err, coef, dcoef = ref_preference(lp, y, spans, ref.double(), 0.2, "sigmoid", 0.0, False)
+    r = L.preference_loss(z.cuda(), y.cuda(), ref.cuda(), beta=0.2, cu_seqlens=torch.tensor(ends, device="cuda"), grad=True)
+    close(r.loss, loss, dl, "loss")
+    close(r.logps, seq, err + 2 * U * seq.abs(), "logps")
+    close_grad(r.dlogits, ref_grad(p, y, coef, 1.0), p, y, coef, dcoef, 1.0, torch.float32, "dlogits")
+
+
 def test_advantages_of_a_sequence_are_expanded_not_copied(L):
     B, S, V = 3, 5, 200
     z, y, gen = make(B * S, V, torch.bfloat16, 2)
@@ -635,6 +697,24 @@ def test_another_stream(L):
         assert torch.equal(x, y)
 
 
+def test_calls_on_two_streams_at_once(L):
+    # each stream has scratch of its own
+    a, b = _inputs(4, 50, 9001, 7), _inputs(4, 60, 9001, 8)
+    want = [_all(L, *x) for x in (a, b)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(20):
+        for k, x in enumerate((a, b)):
+            with torch.cuda.stream(streams[k]):
+                got[k].append(_all(L, *x))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for one in got[k]:
+            for x, y in zip(one, want[k]):
+                assert torch.equal(x, y)
+
+
 def test_captured_calls_replay(L):
     a, b = _inputs(4, 50, 5003, 3), _inputs(4, 50, 5003, 4)
     static = [x.clone() for x in a]
@@ -735,3 +815,33 @@ def test_sequence_offsets_outside_the_rows_are_clamped(L):
     want = L.preference_loss(zg, yg, ref, cu_seqlens=torch.tensor([0, 3, 8], device="cuda"), grad=True)
     got = L.preference_loss(zg, yg, ref, cu_seqlens=torch.tensor([-5, 3, 1 << 40], device="cuda"), grad=True)
     assert torch.equal(want.loss, got.loss) and torch.equal(want.dlogits, got.dlogits)
+
+
+# ----------------------------------------------------------------------------
+# together, under DistributedDataParallel with the compression hook
+# ----------------------------------------------------------------------------
+def test_the_example_trains(gpu_lib):
+    import importlib.util
+    import os
+    import socket
+    from datetime import timedelta
+
+    import torch.distributed as dist
+
+    at = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "train_losses.py")
+    spec = importlib.util.spec_from_file_location("train_losses", at)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    with socket.socket() as s:
+        s.bind(("127.0.0.1", 0))
+        port = s.getsockname()[1]
+    dist.init_process_group("nccl", init_method=f"tcp://127.0.0.1:{port}", rank=0, world_size=1,
+                            timeout=timedelta(seconds=60))
+    try:
+        out = example.main(steps=30)
+    finally:
+        dist.destroy_process_group()
+    assert out["pretrain"][1] < 0.9 * out["pretrain"][0]
+    assert out["distill"][1] < 0.9 * out["distill"][0]
+    assert out["preference"][1] < out["preference"][0] + 0.02       # (starts at log 2, where the reference is)
+    assert out["reward"][1] > out["reward"][0] + 0.05
