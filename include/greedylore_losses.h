@@ -84,7 +84,7 @@ typedef struct {
 } glr_loss_rows;
 
 typedef struct {
-  int64_t seqs;
+  int64_t seqs;                /* in [1, 2^21] */
   const void* cu_seqlens;      /* NULL: the batch entries */
   int32_t cu_type;             /* glr_itype */
 } glr_loss_seqs;

@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(NT + 64) k_distill_row(Rows r, Teach q) {
   float* p_s = zk_s + q.top;
   __shared__ float m_s[NW], s_s[NW], o_s[NW], u_s[NW];
   __shared__ Coefs co;
-  const RowPos p = row_pos(r, blockIdx.x);
+  const RowPos p = row_pos(r, r.first + blockIdx.x);
   int y;
   const bool live = row_target(r, p, y);
   T* dz = r.dz.p ? static_cast<T*>(const_cast<void*>(r.dz.p)) + p.of(r.dz) : nullptr;
@@ -317,8 +317,8 @@ __global__ void __launch_bounds__(NT + 64) k_distill_row(Rows r, Teach q) {
 
 template <class T, bool REST, int TWO, int NT, int NV, bool KEEP>
 void go(const Rows& r, const Teach& q, void* stream) {
-  launch("distillation rows", k_distill_row<T, REST, TWO, NT, NV, KEEP>, r.rows, NT + 64,
-         (bit_words(r.V) + 3 * (size_t)q.top) * 4, stream, r, q);
+  launch_rows("distillation rows", k_distill_row<T, REST, TWO, NT, NV, KEEP>, 1, NT + 64,
+              (bit_words(r.V) + 3 * (size_t)q.top) * 4, stream, r, q);
 }
 
 template <class T, bool REST, int TWO>

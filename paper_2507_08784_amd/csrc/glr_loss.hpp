@@ -30,6 +30,7 @@ constexpr int kMaxTop = 1024;
 constexpr uint32_t kSelfCount = 256;
 constexpr int64_t kMaxLossVocab = (int64_t)1 << 28;
 constexpr int64_t kMaxDistillVocab = (int64_t)1 << 19;   // the list's bitmap stays within 64 KB of LDS
+constexpr int64_t kMaxSeqs = (int64_t)1 << 21;
 constexpr double kRestFloor = 1.0 / (1 << 20);
 constexpr double kMinTemp = 1.0 / (1 << 20);
 
@@ -52,6 +53,7 @@ struct Rows {
   RowArr z, dz, y;
   int64_t ignore;
   uint32_t rows, steps;
+  uint32_t first;   // row of the launch's first workgroup
   int32_t V;
   int32_t y64;
   float c;          // log2(e) / T: exp((z - m) / T) = 2^((z - m) c)
@@ -458,6 +460,17 @@ void launch(const char* what, void (*k)(P...), unsigned grid, unsigned block, si
         }
       },
       t);
+}
+
+// `per` rows a workgroup; a launch has fewer than 2^32 threads
+template <class K, class A>
+void launch_rows(const char* what, K k, unsigned per, unsigned block, size_t lds, void* stream, Rows r, const A& a) {
+  constexpr unsigned most = 1u << 21;      // workgroups of up to 1024 threads
+  for (uint64_t at = 0; at < r.rows; at += (uint64_t)most * per) {
+    const uint64_t left = (r.rows - at + per - 1) / per;
+    r.first = (uint32_t)at;
+    launch(what, k, left < most ? (unsigned)left : most, block, lds, stream, r, a);
+  }
 }
 
 // every row of a call: terms, and the gradient where there is one

@@ -58,9 +58,11 @@ __device__ __forceinline__ double row_terms(const Rows& r, const Terms& a, const
   double term = cut ? -v : -u, slope = cut ? 0.0 : -u, k = 0.0;
   if (a.ref.p) {
     const double d = (double)x.ref - lp, y = expm1(d);
-    k = y - d;
-    term += a.kl * k;
-    slope -= a.kl * y;
+    k = y == INFINITY ? y : y - d;       // (a target of probability 0: inf, not inf - inf)
+    if (a.kl != 0.0) {
+      term += a.kl * k;
+      slope -= a.kl * y;
+    }
   }
   put_shared(a.part + p.t, (float)(x.weight * term));
   put_shared(a.part + (int64_t)r.rows + p.t, (float)(x.weight * k));
@@ -163,7 +165,7 @@ __global__ void __launch_bounds__(NT + 64) k_loss_row(Rows r, Terms a) {
   constexpr int NW = NT / 64;
   __shared__ float m_s[NW], s_s[NW];
   __shared__ float f_s[3];
-  const RowPos p = row_pos(r, blockIdx.x);
+  const RowPos p = row_pos(r, r.first + blockIdx.x);
   int y, seq;
   const bool live = row_live(r, a.seqs, p, y, seq);
   T* dz = r.dz.p ? static_cast<T*>(const_cast<void*>(r.dz.p)) + p.of(r.dz) : nullptr;
@@ -217,7 +219,7 @@ template <class T, int NV, int R>
 __global__ void __launch_bounds__(kLT) k_loss_wave(Rows r, Terms a) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const uint64_t first = ((uint64_t)blockIdx.x * (kLT / 64) + wave) * R;
+  const uint64_t first = r.first + ((uint64_t)blockIdx.x * (kLT / 64) + wave) * R;
   if (first >= r.rows) return;
   const bool mine = lane < R && first + lane < r.rows;      // lane: its row
   const RowPos p = row_pos(r, (uint32_t)first + (mine ? lane : 0));
@@ -269,7 +271,7 @@ __global__ void __launch_bounds__(kLT) k_loss_wave(Rows r, Terms a) {
 // last row to the first (the ones read last are those still in a cache).
 template <class T, int NT, int NV>
 __global__ void __launch_bounds__(NT) k_loss_grad(Rows r, Terms a) {
-  const RowPos p = row_pos(r, r.rows - 1 - blockIdx.x);
+  const RowPos p = row_pos(r, r.rows - 1 - r.first - blockIdx.x);
   int y, seq;
   const bool live = row_live(r, a.seqs, p, y, seq);
   T* dz = static_cast<T*>(const_cast<void*>(r.dz.p)) + p.of(r.dz);
@@ -283,18 +285,17 @@ __global__ void __launch_bounds__(NT) k_loss_grad(Rows r, Terms a) {
 
 template <class T, int NT, int NV, bool KEEP, bool STAY = false>
 void row(const Rows& r, const Terms& a, void* stream) {
-  launch("loss rows", k_loss_row<T, NT, NV, KEEP, STAY>, r.rows, NT + 64, 0, stream, r, a);
+  launch_rows("loss rows", k_loss_row<T, NT, NV, KEEP, STAY>, 1, NT + 64, 0, stream, r, a);
 }
 template <class T, int NV, int R>
 void waves(const Rows& r, const Terms& a, void* stream) {
   // spread over the chip before rows share a wave
   if (R > 1 && r.rows <= 8192) return waves<T, NV, 1>(r, a, stream);
-  constexpr unsigned per = kLT / 64 * R;
-  launch("loss rows of a wave", k_loss_wave<T, NV, R>, (r.rows + per - 1) / per, kLT, 0, stream, r, a);
+  launch_rows("loss rows of a wave", k_loss_wave<T, NV, R>, kLT / 64 * R, kLT, 0, stream, r, a);
 }
 template <class T, int NT, int NV>
 void grad(const Rows& r, const Terms& a, void* stream) {
-  launch("loss gradient rows", k_loss_grad<T, NT, NV>, r.rows, NT, 0, stream, r, a);
+  launch_rows("loss gradient rows", k_loss_grad<T, NT, NV>, 1, NT, 0, stream, r, a);
 }
 
 // A preference loss reads its logits twice.  The last 256 MB of the first

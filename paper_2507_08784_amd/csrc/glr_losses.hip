@@ -65,7 +65,7 @@ __device__ __forceinline__ float pair_terms(const Pairs& q, int i, double L0, in
   if (q.kind == GLR_PREF_SIGMOID) {
     const double soft = log1p(exp(-fabs(h)));
     const double neg = soft + (h < 0.0 ? -h : 0.0), pos = soft + (h > 0.0 ? h : 0.0);   // -log sigma(h), -log sigma(-h)
-    loss = (1.0 - q.smooth) * neg + q.smooth * pos;
+    loss = (1.0 - q.smooth) * neg + (q.smooth > 0.0 ? q.smooth * pos : 0.0);    // (pos may be inf)
     slope = q.beta * (q.smooth - 1.0 / (1.0 + exp(h)));
     if (h != h) loss = h;
   } else if (q.kind == GLR_PREF_HINGE) {
@@ -194,6 +194,7 @@ Rows check_rows(const glr_loss_rows* x, bool need_targets) {
   r.ignore = x->ignore_index;
   r.rows = (uint32_t)(x->batch * x->steps);
   r.steps = (uint32_t)(x->steps > 0 ? x->steps : 1);
+  r.first = 0;
   r.V = (int32_t)x->vocab;
   r.y64 = x->target_type == GLR_I64;
   r.inv_t = 1.0 / x->temperature;
@@ -203,7 +204,7 @@ Rows check_rows(const glr_loss_rows* x, bool need_targets) {
 }
 
 Seqs check_seqs(const glr_loss_rows* x, const glr_loss_seqs& q) {
-  if (q.seqs < 1 || q.seqs >= ((int64_t)1 << 31) - 1) refuse(GLR_ERR_SHAPE, "seqs must be in [1, 2^31 - 2]");
+  if (q.seqs < 1 || q.seqs > kMaxSeqs) refuse(GLR_ERR_SHAPE, "seqs must be in [1, 2^21]");
   if (!q.cu_seqlens) {
     if (q.seqs != x->batch) refuse(GLR_ERR_INVALID_ARG, "seqs must be batch where cu_seqlens is NULL");
   } else {
@@ -261,7 +262,7 @@ glr_status glr_loss_workspace_bytes(const glr_loss_rows* rows, int32_t op, int64
     check_dims(rows);
     if (!bytes) refuse(GLR_ERR_INVALID_ARG, "bytes is NULL");
     if (op < GLR_LOSS_LOGPROBS || op > GLR_LOSS_DISTILL) refuse(GLR_ERR_INVALID_ARG, "unknown op");
-    if (seqs < 0 || seqs >= ((int64_t)1 << 31) - 1) refuse(GLR_ERR_SHAPE, "seqs must be in [0, 2^31 - 2]");
+    if (seqs < 0 || seqs > kMaxSeqs) refuse(GLR_ERR_SHAPE, "seqs must be in [0, 2^21]");
     *bytes = scratch_of(op, rows->batch * rows->steps, seqs, rows->dlogits.data != nullptr).bytes;
   });
 }

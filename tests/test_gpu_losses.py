@@ -237,6 +237,23 @@ def test_unusual_logits_stay_in_their_rows(L, V, dtype, T):
     assert not grads[1, V // 2:].any()
 
 
+def test_impossible_targets_in_losses(L):
+    # log-probability -inf: the terms are the limits, not NaN
+    V = 40
+    z, _, gen = make(4, V, torch.float32, 9, masked=0.0)
+    z[1, 7] = -math.inf
+    y = torch.full((4,), 7)
+    zg, yg, f = z.cuda(), y.cuda(), torch.full((4,), -3.0, device="cuda")
+    r = L.policy_loss(zg, yg, f, torch.ones(4, device="cuda"), ref_logps=f, kl_coef=0.0, grad=True)
+    assert math.isfinite(r.loss) and float(r.kl) == math.inf and not bool(r.dlogits.isnan().any())
+    r = L.policy_loss(zg, yg, f, torch.ones(4, device="cuda"), ref_logps=f, kl_coef=0.1)
+    assert float(r.loss) == math.inf
+    ref = torch.tensor([-3.0, -3.0], device="cuda")
+    for rows, want in (([0, 1], 0.0), ([1, 0], math.inf)):         # the rejected, the chosen one impossible
+        r = L.preference_loss(zg[rows].view(2, 1, V), yg[:2].view(2, 1), ref)
+        assert float(r.loss) == want
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_large_logits_keep_their_differences(L, dtype):
     # 1e4 and more above zero: what counts is the distance to the row's maximum
@@ -735,6 +752,22 @@ def test_captured_calls_replay(L):
         torch.cuda.synchronize()
         for x, y in zip(outs, _all(L, *src)):
             assert torch.equal(x, y), k
+
+
+def test_more_rows_than_one_launch_holds(L):
+    # 2^21 workgroups of 32 rows (of one in the backward pass) and more; a row of two logits
+    rows = (1 << 26) + 5
+    z = torch.randn(rows, 2, device="cuda")
+    y = (torch.arange(rows, device="cuda") % 2)
+    r = L.token_logprobs(z, y, weights=torch.ones(rows, device="cuda"))
+    some = torch.tensor([0, 1, (1 << 26) - 1, 1 << 26, rows - 1], device="cuda")
+    lp, p = ref_rows(z[some].cpu(), y[some].cpu(), 1.0)
+    close(r.logps[some], lp, lp_tol(lp), "logps")
+    d = (z[:, 0] - z[:, 1]) * torch.where(y == 0, 1.0, -1.0)
+    assert bool(((r.logps + torch.log1p(torch.exp(-d.abs())) + (-d).clamp(min=0)).abs() < 1e-4).all())
+    out = L.token_logprobs(z.requires_grad_(True), y).logps      # its backward: a workgroup a row
+    out.sum().backward()
+    assert torch.allclose(z.grad, r.dlogits, rtol=0, atol=4e-5)
 
 
 def test_offsets_beyond_32_bits(L):
