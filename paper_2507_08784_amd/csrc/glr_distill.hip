@@ -50,6 +50,14 @@ __device__ __forceinline__ void row_done(const Rows& r, const Teach& q) {
   if ((threadIdx.x & 63) == 0) *q.loss = (float)(x / n);
 }
 
+// Waves a SIMD that a workgroup of NT threads with the row and one wave beside
+// them asks for, so that two of them share a CU (one reads or writes while the
+// other sums): 80 and 128 registers, which the row's pieces nearly fill.  A
+// few spilled ones cost less than the second workgroup is worth (4000 x 63306
+// bf16 with the rest's mass 312 us alone, 230 with two; 3600 x 84000 with hard
+// labels as well 402 and 288).
+constexpr int two_a_cu(int NT, int NV) { return NT == 704 && NV == 13 ? 6 : NT == 448 && NV == 24 ? 4 : 1; }
+
 // A workgroup a row: the first waves have the row, the last has the teacher's list
 // (its loads, exponentials and logarithms run while the row is on its way, and
 // its fp64 takes no registers beside a row's).  The list's tokens are marked
@@ -59,7 +67,7 @@ __device__ __forceinline__ void row_done(const Rows& r, const Teach& q) {
 // list's own gradient elements are written over the dense ones behind a
 // barrier.
 template <class T, bool REST, int TWO, int NT, int NV, bool KEEP>
-__global__ void __launch_bounds__(NT + 64) k_distill_row(Rows r, Teach q) {
+__global__ void __launch_bounds__(NT + 64, two_a_cu(NT, NV)) k_distill_row(Rows r, Teach q) {
   constexpr int N = Piece<T>::N, NW = NT / 64;
   extern __shared__ uint32_t bits[];
   const int words = (r.V + 8 + 31) / 32;
@@ -332,6 +340,7 @@ void rows_of(const Rows& r, const Teach& q, void* stream) {
   if (n <= 5632) return go<T, REST, TWO, 704, 8, true>(r, q, stream);
   if (n <= 7040) return go<T, REST, TWO, 704, 10, true>(r, q, stream);
   if (n <= 9152) return go<T, REST, TWO, 704, 13, true>(r, q, stream);
+  if (n <= 10752) return go<T, REST, TWO, 448, 24, true>(r, q, stream);
   if (n <= 13440) return go<T, REST, TWO, 960, 14, true>(r, q, stream);
   if (n <= 16320) return go<T, REST, TWO, 960, 17, true>(r, q, stream);
   return go<T, REST, TWO, 960, 8, false>(r, q, stream);
