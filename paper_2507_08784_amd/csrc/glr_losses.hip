@@ -85,28 +85,38 @@ __device__ __forceinline__ float pair_terms(const Pairs& q, int i, double L0, in
   return (float)loss;
 }
 
-// A workgroup a pair; the last one adds the pairs' losses.
+// A workgroup a pair, half of it a sequence; the last one adds the pairs' losses.
 __global__ void __launch_bounds__(1024) k_loss_pairs(Rows r, Pairs q) {
-  __shared__ double shd[16];
-  __shared__ int shi[16];
+  __shared__ double L_s[16];
+  __shared__ int n_s[16];
   const int half = q.seqs.n >> 1;
-  double L[2];
-  int n[2];
-  for (int side = 0; side < 2; ++side) {
-    uint32_t lo, hi;
-    seq_span(r, q.seqs, (int64_t)blockIdx.x + side * (int64_t)half, lo, hi);
-    double x = 0.0;
-    int c = 0;
-    for (uint64_t t = (uint64_t)lo + threadIdx.x; t < hi; t += 1024) {
-      int y;
-      if (q.average) c += row_target(r, row_pos(r, (uint32_t)t), y);
-      x += q.lp[t];                                                    // (0 where masked)
-    }
-    L[side] = block_sum<1024, double>(x, shd);
-    n[side] = q.average ? block_sum<1024, int>(c, shi) : 1;
+  uint32_t lo, hi;
+  seq_span(r, q.seqs, (int64_t)blockIdx.x + (int64_t)(threadIdx.x >> 9) * half, lo, hi);
+  double x = 0.0;
+  int c = 0;
+  for (uint64_t t = (uint64_t)lo + (threadIdx.x & 511); t < hi; t += 512) {
+    int y;
+    if (q.average) c += row_target(r, row_pos(r, (uint32_t)t), y);
+    x += q.lp[t];                                                      // (0 where masked)
   }
+  x = wave_sum(x);
+  c = wave_sum(c);
+  if ((threadIdx.x & 63) == 0) {
+    L_s[threadIdx.x >> 6] = x;
+    n_s[threadIdx.x >> 6] = c;
+  }
+  __syncthreads();
   if (threadIdx.x >= 64) return;
-  if (threadIdx.x == 0) put_shared(q.part + blockIdx.x, pair_terms(q, blockIdx.x, L[0], n[0], L[1], n[1]));
+  if (threadIdx.x == 0) {
+    double L[2] = {0.0, 0.0};
+    int n[2] = {0, 0};
+    for (int w = 0; w < 16; ++w) {
+      L[w >> 3] += L_s[w];
+      n[w >> 3] += n_s[w];
+    }
+    if (!q.average) n[0] = n[1] = 1;
+    put_shared(q.part + blockIdx.x, pair_terms(q, blockIdx.x, L[0], n[0], L[1], n[1]));
+  }
   if (last_to_arrive(q.sync, gridDim.x)) {
     const double loss = total_of(q.part, gridDim.x);
     if (threadIdx.x == 0) *q.loss = (float)(loss / half);
