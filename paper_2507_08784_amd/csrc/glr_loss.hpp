@@ -181,19 +181,6 @@ __device__ __forceinline__ X wave_sum(X x) {
   x += dpp_move<0x143, 0xC>(X(0), x);
   return lane_value(x, 63);
 }
-template <int NT>
-__device__ __forceinline__ float block_max(float x, float* sh) {
-  x = wave_max(x);
-  if constexpr (NT > 64) {
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = sh[0];
-#pragma unroll
-    for (int w = 1; w < NT / 64; ++w) x = fmaxf(x, sh[w]);
-  }
-  return x;
-}
 template <int NT, class X>
 __device__ __forceinline__ X block_sum(X x, X* sh) {
   x = wave_sum(x);

@@ -9,6 +9,7 @@
 
 #include <cmath>
 #include <string>
+#include <utility>
 
 #include "glr_loss.hpp"
 
@@ -185,6 +186,18 @@ void check_dims(const glr_loss_rows* x) {
   if (x->dtype < GLR_F32 || x->dtype > GLR_F16) refuse(GLR_ERR_INVALID_ARG, "unknown logits type");
 }
 
+// rows of dlogits that overlap would be written by several workgroups at once
+void check_apart(const glr_loss_rows* x) {
+  int64_t n0 = x->batch, s0 = x->dlogits.stride_b, n1 = x->steps, s1 = x->dlogits.stride_s;
+  if (n1 < 2 || (n0 > 1 && s0 < s1)) {
+    std::swap(n0, n1);
+    std::swap(s0, s1);
+  }
+  // s1 is the shorter stride of a dimension of more than one, if there is one
+  const __int128 inner = n1 > 1 ? (__int128)s1 * (n1 - 1) + x->vocab : x->vocab;
+  if ((n1 > 1 && s1 < x->vocab) || (n0 > 1 && s0 < inner)) refuse(GLR_ERR_INVALID_ARG, "rows of dlogits overlap");
+}
+
 Rows check_rows(const glr_loss_rows* x, bool need_targets) {
   check_dims(x);
   if (x->target_type != GLR_I32 && x->target_type != GLR_I64) refuse(GLR_ERR_INVALID_ARG, "unknown target type");
@@ -194,7 +207,10 @@ Rows check_rows(const glr_loss_rows* x, bool need_targets) {
   const size_t es = x->dtype == GLR_F32 ? 4 : 2;
   if (x->batch * x->steps > 0) {
     check_array(x->logits, es, "logits");
-    if (x->dlogits.data) check_array(x->dlogits, es, "dlogits");
+    if (x->dlogits.data) {
+      check_array(x->dlogits, es, "dlogits");
+      check_apart(x);
+    }
     if (need_targets) check_array(x->targets, x->target_type == GLR_I64 ? 8 : 4, "targets");
   }
   Rows r;

@@ -813,6 +813,8 @@ def test_refusals(L, gpu_lib):
         L.token_logprobs(z, y, weights=f, out=z.half())
     with pytest.raises(ValueError, match="strides"):
         L.token_logprobs(z[:2], y[:2], weights=f[:2], out=z.as_strided((2, 9), (18, 1)))
+    with pytest.raises(gpu_lib.GlrError, match="overlap"):
+        L.token_logprobs(z, y, weights=f, out=torch.zeros(1, 9, device="cuda").expand(4, 9))
     with pytest.raises(gpu_lib.GlrError, match="temperature"):
         L.token_logprobs(z, y, temperature=0.0)
     with pytest.raises(ValueError, match="cu_seqlens"):

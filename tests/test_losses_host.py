@@ -141,7 +141,9 @@ NAN, INF = float("nan"), float("inf")
     (dict(vocab=(1 << 28) + 1), 2), (dict(dtype=3), 1), (dict(dtype=-1), 1), (dict(target_type=2), 1),
     (dict(temperature=0.0), 1), (dict(temperature=NAN), 1), (dict(temperature=INF), 1), (dict(temperature=-1.0), 1),
     (dict(grad_scale=INF), 1), (dict(logits=(None, 0, 0)), 1), (dict(logits=(PTR + 2, 150, 50)), 1),
-    (dict(dlogits=(PTR + 1, 150, 50)), 1), (dict(targets=(None, 0, 0)), 1), (dict(targets=(PTR + 4, 3, 1)), 1),
+    (dict(dlogits=(PTR + 1, 150, 50)), 1), (dict(dlogits=(PTR, 150, 49)), 1), (dict(dlogits=(PTR, 149, 50)), 1),
+    (dict(dlogits=(PTR, 0, 50)), 1), (dict(dlogits=(PTR, 50, 99)), 1), (dict(dlogits=(PTR, 49, 100)), 1),
+    (dict(dlogits=(PTR, 150, -50)), 1), (dict(targets=(None, 0, 0)), 1), (dict(targets=(PTR + 4, 3, 1)), 1),
 ])
 def test_bad_rows_are_refused_by_every_entry(kw, code):
     lib, r = _lib(), _rows(**kw)
@@ -152,6 +154,15 @@ def test_bad_rows_are_refused_by_every_entry(kw, code):
     assert lib.glr_policy_loss(r, _policy(), *WS, None) == code
     if "targets" not in kw or kw["targets"][0]:     # distillation does without targets
         assert lib.glr_distill_loss(r, _distill(), *WS, None) == code
+
+
+@pytest.mark.parametrize("shape,strides", [((2, 3), (150, 50)), ((2, 3), (50, 100)), ((2, 3), (160, 52)), ((1, 3), (0, 50)),
+                                           ((3, 1), (50, 0)), ((1, 1), (0, 0)), ((1, 3), (7, 50)), ((3, 1), (50, 7))])
+def test_rows_of_a_gradient_that_lie_apart_are_taken(shape, strides):
+    # (without weights the call is refused for those, after its rows were accepted)
+    r = _rows(batch=shape[0], steps=shape[1], dlogits=(PTR, *strides))
+    assert _lib().glr_token_logprobs(r, None, PTR, None, None, 0, None) == 1
+    assert b"weights" in _lib().glr_last_error(None)
 
 
 def test_null_structs_and_outputs_are_refused():
@@ -206,7 +217,7 @@ def test_bad_distillation_arguments_are_refused(kw, code):
 
 def test_distillation_limits():
     lib = _lib()
-    assert lib.glr_distill_loss(_rows(vocab=(1 << 19) + 1), _distill(), *WS, None) == 2
+    assert lib.glr_distill_loss(_rows(vocab=(1 << 19) + 1, dlogits=(None, 0, 0)), _distill(), *WS, None) == 2
     assert lib.glr_distill_loss(_rows(targets=(None, 0, 0)), _distill(hard_weight=0.5), *WS, None) == 1
 
 
