@@ -23,7 +23,9 @@ The gradient with respect to the logits comes in one of two ways:
              (one pass over the logits gives both) and backward hands it on,
              times the upstream gradient (a factor other than a power of two
              rounds bf16 and fp16 gradients a second time: pass it as
-             `grad_scale` instead, with which the gradient is made)
+             `grad_scale` instead, with which the gradient is made; an fp16
+             gradient without one waits for backward times a power of two about
+             the number it is averaged over, so that a loss scaler finds it whole)
   explicit   grad=True (weights=... of token_logprobs) returns it as `dlogits`;
              nothing is recorded
 
@@ -66,8 +68,13 @@ def _call(name, logits, *args, scratch=True):
         _native = {n: getattr(_losses, n) for n in dir(_losses) if not n.startswith("_")}
     stream = capturing = None
     if isinstance(logits, torch.Tensor) and logits.is_cuda:      # (the binding refuses the others)
-        stream = torch._C._cuda_getCurrentRawStream(logits.device.index)
-        capturing = torch._C._cuda_isCurrentStreamCapturing()
+        index = logits.device.index
+        stream = torch._C._cuda_getCurrentRawStream(index)
+        if index == torch._C._cuda_getDevice():
+            capturing = torch._C._cuda_isCurrentStreamCapturing()
+        else:
+            with torch.cuda.device(index):
+                capturing = torch._C._cuda_isCurrentStreamCapturing()
     r = _native[name](stream, capturing, logits, *args) if scratch else _native[name](stream, logits, *args)
     if type(r) is int:
         _check(r)
@@ -82,14 +89,24 @@ def _records(logits, grad):
 # ----------------------------------------------------------------------------
 # autograd
 # ----------------------------------------------------------------------------
+def _ahead(logits, record, count, grad_scale):
+    """What a recorded gradient is multiplied by as it is made, and divided by
+    as it is handed on: in fp16 a mean over many rows would lie below the
+    smallest values, and a scaler's factor comes only with backward.  A
+    grad_scale of the caller's stands as it is."""
+    if record and logits.dtype == torch.float16 and count > 1 and grad_scale == 1.0:
+        return 2.0 ** (int(count).bit_length() - 1)
+    return 1.0
+
+
 class _WithGradient(torch.autograd.Function):
     """A loss whose gradient came with it; backward hands it on once, times
     the upstream gradient."""
 
     @staticmethod
-    def forward(ctx, logits, compute):
+    def forward(ctx, logits, compute, ahead):
         result = compute()
-        ctx.dlogits = result.dlogits
+        ctx.dlogits, ctx.ahead = result.dlogits, ahead
         rest = tuple(result[1:-1])
         ctx.mark_non_differentiable(*rest)
         return (result.loss,) + rest
@@ -100,12 +117,12 @@ class _WithGradient(torch.autograd.Function):
         d, ctx.dlogits = ctx.dlogits, None
         if d is None:
             raise RuntimeError("the loss's gradient was handed on already: call the loss again for a second backward")
-        scale = grad_loss.float().contiguous()
+        scale = (grad_loss.float() / ctx.ahead if ctx.ahead != 1.0 else grad_loss.float()).contiguous()
         if d.is_contiguous():
             _call("rescale", d, scale, scratch=False)
         else:                       # an `out` with room between its rows
             d.mul_(scale)
-        return d, None
+        return d, None, None
 
 
 class _TokenLogprobs(torch.autograd.Function):
@@ -155,13 +172,15 @@ def preference_loss(logits, targets, ref_logps, *, beta=0.1, kind="sigmoid", lab
     grad = bool(grad)
     record = _records(logits, grad)
 
+    ahead = _ahead(logits, record, ref_logps.numel() // 2 if record and isinstance(ref_logps, torch.Tensor) else 0, grad_scale)
+
     def compute():
         return PreferenceLoss._make(_call(
-            "preference", logits, targets, ignore_index, grad or record, grad_scale, out, ref_logps, beta, KINDS[kind],
+            "preference", logits, targets, ignore_index, grad or record, grad_scale * ahead, out, ref_logps, beta, KINDS[kind],
             label_smoothing, bool(average), cu_seqlens, 1.0))
 
     if record:
-        return PreferenceLoss(*_WithGradient.apply(logits, compute), None)
+        return PreferenceLoss(*_WithGradient.apply(logits, compute, ahead), None)
     return compute()
 
 
@@ -183,13 +202,15 @@ def policy_loss(logits, targets, old_logps, advantages, *, ref_logps=None, clip_
     grad = bool(grad)
     record = _records(logits, grad)
 
+    ahead = _ahead(logits, record, logits.shape[:-1].numel() if record else 0, grad_scale)
+
     def compute():
         return PolicyLoss._make(_call(
-            "policy", logits, targets, ignore_index, temperature, grad or record, grad_scale, out, old_logps, advantages,
+            "policy", logits, targets, ignore_index, temperature, grad or record, grad_scale * ahead, out, old_logps, advantages,
             ref_logps, clip_low, clip_high, kl_coef, REDUCTIONS[reduction], denominator or 0.0, cu_seqlens))
 
     if record:
-        return PolicyLoss(*_WithGradient.apply(logits, compute), None)
+        return PolicyLoss(*_WithGradient.apply(logits, compute, ahead), None)
     return compute()
 
 
@@ -212,11 +233,13 @@ def distill_loss(logits, teacher_ids, teacher_logits, *, temperature=1.0, teache
     grad = bool(grad)
     record = _records(logits, grad)
 
+    ahead = _ahead(logits, record, logits.shape[:-1].numel() if record else 0, grad_scale)
+
     def compute():
         return DistillLoss._make(_call(
-            "distill", logits, targets, ignore_index, temperature, grad or record, grad_scale, out, teacher_ids,
+            "distill", logits, targets, ignore_index, temperature, grad or record, grad_scale * ahead, out, teacher_ids,
             teacher_logits, teacher_lse, hard_weight, denominator or 0.0))
 
     if record:
-        return DistillLoss(*_WithGradient.apply(logits, compute), None)
+        return DistillLoss(*_WithGradient.apply(logits, compute, ahead), None)
     return compute()

@@ -498,6 +498,30 @@ def test_many_pairs(L):
     close_grad(r.dlogits, ref_grad(p, y, coef, 1.0), p, y, coef, dcoef, 1.0, torch.float32, "dlogits")
 
 
+def test_fp16_gradients_survive_until_a_loss_scaler_multiplies_them(L):
+    # averaged over 4096 rows most elements lie below fp16's smallest value;
+    # made with the scale, or recorded (times the power of two in the number of
+    # rows, or pairs) and scaled in backward, they are the same up to a second
+    # rounding, and up to what a subnormal element lost before the scale
+    B, S, V, scale = 32, 128, 600, 2.0 ** 16
+    z, y, gen = make(B * S, V, torch.float16, 21)
+    zg, yg = z.cuda().view(B, S, V), y.cuda().view(B, S)
+    f = torch.full((B, S), -6.0, device="cuda")
+    adv = torch.randn(B, S, generator=gen).cuda()
+    ids = torch.stack([torch.randperm(V, generator=gen)[:4] for _ in range(B * S)]).cuda().view(B, S, 4)
+    t = torch.randn(B, S, 4, generator=gen).cuda()
+    base = torch.full((B,), -600.0, device="cuda")
+    calls = [(lambda x, **k: L.policy_loss(x, yg, f, adv, **k), 4096),
+             (lambda x, **k: L.distill_loss(x, ids, t, targets=yg, **k), 4096),
+             (lambda x, **k: L.preference_loss(x, yg, base, beta=0.1, **k), 16)]
+    for call, ahead in calls:
+        want = call(zg, grad=True, grad_scale=scale).dlogits.double()
+        leaf = zg.clone().requires_grad_(True)
+        (call(leaf).loss * scale).backward()
+        off = (leaf.grad.double() - want).abs()
+        assert bool((off <= 2.0 ** -10 * want.abs() + 2.0 ** -25 * scale / ahead + 2.0 ** -24).all())
+
+
 def test_advantages_of_a_sequence_are_expanded_not_copied(L):
     B, S, V = 3, 5, 200
     z, y, gen = make(B * S, V, torch.bfloat16, 2)
